@@ -43,7 +43,10 @@ typedef enum radix_status {
     RADIX_ERR_BAD_TOKEN = -7,         /* device data: token id < 0 or >= vocab, position id or row index out of range */
     RADIX_ERR_HIP = -8,               /* a HIP runtime call failed */
     RADIX_ERR_BAD_CONFIG = -9,        /* inconsistent model configuration */
-    RADIX_ERR_STATIC_LIMIT = -10      /* radix_build_index_static: more sequences than its static scratch array holds */
+    RADIX_ERR_STATIC_LIMIT = -10,     /* radix_build_index_static: more sequences than its static scratch array holds */
+    RADIX_ERR_BAD_PAGE = -11,         /* device data: a cache position without a page, a page id out of range or listed twice */
+    RADIX_ERR_OUT_OF_PAGES = -12,     /* device data: no free page left, or a sequence longer than its row of the page table */
+    RADIX_ERR_BAD_SLOT = -13          /* device data: a cache slot out of range, listed twice, or not empty where it has to be */
 } radix_status;
 
 typedef enum radix_dtype { RADIX_F32 = 0, RADIX_BF16 = 1, RADIX_F16 = 2 } radix_dtype;
@@ -302,6 +305,174 @@ int radix_lm_head(const radix_model* model, const float* hidden, int32_t n_src_r
  */
 int radix_index_select_rows(const void* src, int32_t n_src_rows, const int32_t* idx, int32_t n_rows,
                             size_t row_bytes, void* dst, int32_t* status_dev, void* stream);
+
+/*
+ * Paged key/value cache.  radix_cache is a HOST struct of device pointers; the caller allocates and owns everything
+ * in it, and every call takes it as it is (nothing is kept between calls).
+ *   pages       [n_layers][n_pages][2][n_kv_heads][page_size][head_dim] in `dtype`: keys (0) and values (1), 16-byte
+ *               aligned, radix_cache_bytes bytes.  A cache for a model has its layers, kv heads, head size and
+ *               compute_dtype.  Shapes: page_size 16, 32, 64, 128 or 256; head_dim 128 with 16-bit types, a multiple of
+ *               4 up to 128 with RADIX_F32.
+ *   page_refs   int32[n_pages]  number of table entries that hold the page; 0 = free
+ *   page_table  int32[max_seqs][max_pages]  entry i of a row: the page with positions i * page_size ..; -1 = none
+ *   seq_lens    int32[max_seqs]  positions in the cache.  A row of length n holds its pages in its first
+ *               ceil(n / page_size) entries.
+ * A row of the table is a "slot": where a sequence lives between calls.  The calls take the slots of a batch as a list
+ * (`slots`; NULL: slot b for entry b).  Page numbers are given out lowest first, in the order of the list, so that every
+ * result is a function of the state before the call.  Lists have at most RADIX_CACHE_MAX_LIST entries.
+ *
+ * Errors in device data go to *status_dev (may be NULL; first error wins; the caller clears it).  extend, fork and copy are
+ * all or nothing: on an error nothing has changed.
+ */
+#define RADIX_CACHE_MAX_LIST 65535
+typedef struct radix_cache {
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page_size;   /* positions of a page */
+    int32_t n_pages;
+    int32_t dtype;       /* radix_dtype */
+    int32_t max_seqs;
+    int32_t max_pages;   /* entries of a table row; max_pages * page_size < 2^31 */
+    void* pages;
+    int32_t* page_refs;
+    int32_t* page_table;
+    int32_t* seq_lens;
+} radix_cache;
+
+/* Bytes of `pages` / of the workspace of the page calls with lists of up to max_n entries (256-byte aligned; compact: 0).
+ * Only the sizes of the struct are read. */
+int radix_cache_bytes(const radix_cache* cache, size_t* bytes_out);
+int radix_cache_workspace_bytes(const radix_cache* cache, int32_t max_n, size_t* bytes_out);
+
+/* Empties the cache: all pages free, no entries, lengths 0 (what `pages` holds stays). */
+int radix_cache_reset(const radix_cache* cache, void* stream);
+
+/*
+ * radix_cache_extend - room for the next cu_seqlens[b+1] - cu_seqlens[b] tokens of slot slots[b], b < B: the length grows
+ * by that, the pages that it needs are taken, and past[b] becomes the length before.  radix_cache_append then stores the
+ * tokens' keys and values layer by layer, radix_paged_attention attends to them.  A last page that is partly filled and
+ * shared with another slot is replaced by a copy first.
+ * Errors: RADIX_ERR_BAD_CU_SEQLENS (not 0 .. non-decreasing), RADIX_ERR_BAD_SLOT (out of range or listed twice),
+ * RADIX_ERR_OUT_OF_PAGES (also: longer than max_pages * page_size), RADIX_ERR_BAD_PAGE (a length or an entry that cannot
+ * be); then past[b] = -1 for all b, with which append stores nothing and attention gives zeros.
+ */
+int radix_cache_extend(const radix_cache* cache, const int32_t* slots, const int32_t* cu_seqlens, int32_t B, int32_t* past,
+                       void* ws, size_t ws_bytes, int32_t* status_dev, void* stream);
+
+/*
+ * radix_cache_fork - slot children[i] (empty) becomes what slot parents[i] is, i < n: full pages are shared, a partly
+ * filled last page is copied (its filled rows, all layers).  A parent may have many children in one call.
+ * Errors: RADIX_ERR_BAD_SLOT (out of range; a child that is not empty, is listed twice or is a parent too),
+ * RADIX_ERR_OUT_OF_PAGES, RADIX_ERR_BAD_PAGE.
+ */
+int radix_cache_fork(const radix_cache* cache, const int32_t* parents, const int32_t* children, int32_t n, void* ws,
+                     size_t ws_bytes, int32_t* status_dev, void* stream);
+
+/*
+ * radix_cache_free - slot slots[i] is cut to its first keep_lens[i] positions (NULL, or negative: none), i < n; pages that
+ * it holds behind them are given back, and are free once no other slot holds them.  A length that is not longer stays.  A
+ * slot may be listed twice (the shorter length counts).  Entries that cannot be are reported and dropped.
+ */
+int radix_cache_free(const radix_cache* cache, const int32_t* slots, const int32_t* keep_lens, int32_t n, int32_t* status_dev,
+                     void* stream);
+
+/*
+ * radix_cache_compact - moves used pages until they are pages 0 .. n_used - 1 (n_used: int32[1], out): those numbered
+ * n_used or more move, in ascending order, into the free ones below, ascending; the table follows.  The rest of every
+ * layer's pages is free then, e.g. to be given up in a smaller cache.
+ */
+int radix_cache_compact(const radix_cache* cache, int32_t* n_used, void* ws, size_t ws_bytes, int32_t* status_dev, void* stream);
+
+/*
+ * radix_cache_copy_pages - copies page src[i] to page dst[i] in all layers, i < n; counts and table stay.  For callers with a
+ * page management of their own.  A page id out of range, a destination that is listed twice or is a source too:
+ * RADIX_ERR_BAD_PAGE, nothing is copied.
+ */
+int radix_cache_copy_pages(const radix_cache* cache, const int32_t* src, const int32_t* dst, int32_t n, void* ws, size_t ws_bytes,
+                           int32_t* status_dev, void* stream);
+
+/*
+ * radix_cache_append - stores keys and values of new tokens in one layer: token i of sequence b (cu_seqlens[b] <= i <
+ * cu_seqlens[b+1]) goes to position past[b] + i - cu_seqlens[b] of its slot (past[b] < 0: nowhere).
+ *   k, v          [N][n_kv_heads][head_dim] in the cache's dtype; tokens k_stride / v_stride ELEMENTS apart (so that they may
+ *                 lie in fused q | k | v rows), 16-byte aligned, strides multiples of 16 bytes
+ *   cu_seqlens    int32[B+1]; rows from cu_seqlens[B] on belong to no sequence and are ignored
+ * A position without a page (RADIX_ERR_BAD_PAGE), a slot out of range (RADIX_ERR_BAD_SLOT) or a range outside [0, N)
+ * (RADIX_ERR_BAD_CU_SEQLENS): the token is left out and reported.
+ */
+int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                       const int32_t* cu_seqlens, const int32_t* past, const int32_t* slots, int32_t B, int32_t N,
+                       int32_t* status_dev, void* stream);
+
+/*
+ * radix_paged_attention - causal attention of new tokens over the cache, their own keys and values included: token i of
+ * sequence b sees positions 0 .. past[b] + i - cu_seqlens[b] of slot slots[b].  Any mix of chunks and single tokens.
+ *   q, out        [N][n_q_heads][head_dim] in the cache's dtype, tokens q_stride / out_stride elements apart; n_q_heads a
+ *                 multiple of n_kv_heads (query head h reads kv head h / (n_q_heads / n_kv_heads)); alignment as above;
+ *                 scores are scaled by 1 / sqrt(head_dim)
+ *   max_new       >= tokens of any sequence of the call (host value, sizes the grid)
+ *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new), 256-byte aligned
+ * past[b] < 0: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position are not
+ * read; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).
+ * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values.
+ * A sequence whose range is not in [0, N) or longer than max_new (RADIX_ERR_BAD_CU_SEQLENS) is left out; a slot out of
+ * range (RADIX_ERR_BAD_SLOT) or more positions than a table row holds (RADIX_ERR_BAD_PAGE): zeros; a table entry that is no
+ * page is read as page 0 (RADIX_ERR_BAD_PAGE).  N * n_q_heads < 2^31.
+ */
+int radix_paged_attention_workspace_bytes(const radix_cache* cache, int32_t n_q_heads, int32_t max_N, int32_t max_B,
+                                          int32_t max_new, size_t* bytes_out);
+int radix_paged_attention(const radix_cache* cache, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,
+                          const int32_t* cu_seqlens, const int32_t* past, const int32_t* slots, int32_t B, int32_t N,
+                          int32_t max_new, void* out, int64_t out_stride, void* ws, size_t ws_bytes, int32_t* status_dev,
+                          void* stream);
+
+/*
+ * radix_extend_forward - forward of new tokens behind what a cache holds: a chunk of a prompt, the next token of a generation, or
+ * both in one batch.  Runs radix_cache_extend for the batch, then the layers over the N new tokens at positions past[b] + offset,
+ * storing their keys and values and attending over the cache.
+ *   tok           int32[N], cu_seqlens int32[B+1] (0 .. N), slots int32[B] or NULL, max_new >= new tokens of any sequence
+ *   out           float[N, d]: final-RMSNorm hidden states, as from radix_prefill_forward
+ *   ws            at least radix_extend_workspace_bytes(model, cache, N, B, max_new), 256-byte aligned
+ * The cache holds keys, values and attention outputs in compute_dtype: a leading (hi, lo) layer (hilo_layers) keeps pairs for its
+ * GEMM inputs only, not for q, k, v and the attention output.  A sequence may hold min(max_pages * page_size, max_pos) positions.
+ * RADIX_ERR_BAD_CONFIG: the cache is not of the model's shape.  Device-data errors: radix_device_status(ws); where the cache could
+ * not be extended (codes of radix_cache_extend) it has not changed, and out holds nothing of use.  Asynchronous on `stream`; can be
+ * captured into a graph (replays extend the cache again).
+ */
+int radix_extend_workspace_bytes(const radix_model* model, const radix_cache* cache, int32_t max_N, int32_t max_B, int32_t max_new,
+                                 size_t* bytes_out);
+int radix_extend_forward(const radix_model* model, const radix_cache* cache, const int32_t* tok, const int32_t* cu_seqlens,
+                         const int32_t* slots, int32_t B, int32_t N, int32_t max_new, float* out, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/*
+ * radix_token_logprobs - of every row x of logits[n_rows, vocab] (dtype any radix_dtype, rows row_stride elements apart):
+ *   logprobs      float[n_rows, n_given]: log softmax(x)[given[r, j]]; given < 0: 0 (no token); >= vocab: NaN, and
+ *                 RADIX_ERR_BAD_TOKEN in *status_dev
+ *   entropy       float[n_rows] or NULL: - sum p log p (natural logarithm)
+ *   top_ids, top_logprobs  int32 / float[n_rows, top_k]: the top_k <= RADIX_MAX_TOP_K likeliest tokens, likeliest first, equal
+ *                 logits by the lower id
+ * Logits of -inf (tokens that are ruled out) have no part in the sums.  A row without a finite logit, or with a NaN or +inf, has
+ * NaN for logprobs, entropy and top_logprobs; its ids are ordered as ever, a NaN last.  n_given, top_k may be 0 (pointers NULL then).
+ * Sums are fp32; how a row is summed depends on n_rows and vocab only.
+ */
+#define RADIX_MAX_TOP_K 32
+int radix_token_logprobs_workspace_bytes(int32_t max_rows, int32_t vocab, int32_t n_given, int32_t top_k, size_t* bytes_out);
+int radix_token_logprobs(const void* logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab, const int32_t* given,
+                         int32_t n_given, int32_t top_k, float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs,
+                         void* ws, size_t ws_bytes, int32_t* status_dev, void* stream);
+
+/*
+ * radix_score_tokens - radix_lm_head and radix_token_logprobs in one call, RADIX_SCORE_ROWS rows at a time, so that the logits of
+ * whole documents never exist at once.  Arguments as for the two; needs a model with an LM head.  The status word of `ws` reports
+ * row indices and tokens out of range.
+ */
+#define RADIX_SCORE_ROWS 512
+int radix_score_tokens_workspace_bytes(const radix_model* model, int32_t max_rows, int32_t n_given, int32_t top_k, size_t* bytes_out);
+int radix_score_tokens(const radix_model* model, const float* hidden, int32_t n_src_rows, const int32_t* rows, int32_t n_rows,
+                       const int32_t* given, int32_t n_given, int32_t top_k, float* logprobs, float* entropy, int32_t* top_ids,
+                       float* top_logprobs, void* ws, size_t ws_bytes, void* stream);
 
 /* Waits for `stream` and returns the device-data status recorded in the workspace by the most
  * recent radix_build_index / radix_prefill_forward* call that used it (each call starts by

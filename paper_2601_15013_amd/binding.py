@@ -24,6 +24,10 @@ EXPORTS = (
     "radix_dedup_decision",
     "radix_lm_head_workspace_bytes", "radix_lm_head",
     "radix_index_select_rows", "radix_device_status", "radix_status_string",
+    "radix_cache_bytes", "radix_cache_workspace_bytes", "radix_cache_reset", "radix_cache_extend", "radix_cache_fork", "radix_cache_free",
+    "radix_cache_compact", "radix_cache_copy_pages", "radix_cache_append", "radix_paged_attention_workspace_bytes", "radix_paged_attention",
+    "radix_extend_workspace_bytes", "radix_extend_forward", "radix_token_logprobs_workspace_bytes", "radix_token_logprobs",
+    "radix_score_tokens_workspace_bytes", "radix_score_tokens",
     "radix_timing_enable", "radix_timing_collect", "radix_debug_gemm_tile", "radix_debug_gemm_band", "radix_debug_gemm_plan", "radix_debug_gemm_plan_cus",
     "radix_debug_gemm_plan_us", "radix_debug_gemm_plan_folded",
     "radix_debug_index_first_round", "radix_debug_index_host_slots", "radix_debug_gemm_run", "radix_debug_gemm_run_folded",
@@ -57,6 +61,11 @@ class radix_weights(C.Structure):
 class radix_fwd_opts(C.Structure):
     _fields_ = [("threshold", C.c_float), ("force_dedup", C.c_int32), ("attention_mode", C.c_int32),
                 ("pad_compact_to", C.c_int32)]
+
+
+class radix_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_kv_heads", "head_dim", "page_size", "n_pages", "dtype", "max_seqs",
+                                          "max_pages")] + [(n, C.c_void_p) for n in ("pages", "page_refs", "page_table", "seq_lens")]
 
 
 _LIB: Optional[C.CDLL] = None
@@ -99,6 +108,24 @@ def _lib() -> C.CDLL:
                                                     [C.c_float] * 2 + [vp] * 4)
         lib.radix_debug_gemm_plan_us.argtypes = [i32] * 7 + [C.POINTER(C.c_double)]
         lib.radix_debug_index_first_round.argtypes = [i32] * 2
+        cache, i64, szp = C.POINTER(radix_cache), C.c_int64, C.POINTER(sz)
+        lib.radix_cache_bytes.argtypes = [cache, szp]
+        lib.radix_cache_workspace_bytes.argtypes = [cache, i32, szp]
+        lib.radix_cache_reset.argtypes = [cache, vp]
+        lib.radix_cache_extend.argtypes = [cache, vp, vp, i32, vp, vp, sz, vp, vp]
+        lib.radix_cache_fork.argtypes = [cache, vp, vp, i32, vp, sz, vp, vp]
+        lib.radix_cache_free.argtypes = [cache, vp, vp, i32, vp, vp]
+        lib.radix_cache_compact.argtypes = [cache, vp, vp, sz, vp, vp]
+        lib.radix_cache_copy_pages.argtypes = [cache, vp, vp, i32, vp, sz, vp, vp]
+        lib.radix_cache_append.argtypes = [cache, i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, vp, vp]
+        lib.radix_paged_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, szp]
+        lib.radix_paged_attention.argtypes = [cache, i32, vp, i64, i32, vp, vp, vp, i32, i32, i32, vp, i64, vp, sz, vp, vp]
+        lib.radix_extend_workspace_bytes.argtypes = [vp, cache, i32, i32, i32, szp]
+        lib.radix_extend_forward.argtypes = [vp, cache, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        lib.radix_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32, szp]
+        lib.radix_token_logprobs.argtypes = [vp, i32, i64, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp, vp]
+        lib.radix_score_tokens_workspace_bytes.argtypes = [vp, i32, i32, i32, szp]
+        lib.radix_score_tokens.argtypes = [vp, vp, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         lib.radix_status_string.argtypes = [C.c_int]
         lib.radix_status_string.restype = C.c_char_p
         for n in EXPORTS:
@@ -326,6 +353,276 @@ def radix_index_select_rows(src: torch.Tensor, idx: torch.Tensor, out: Optional[
     rc = _lib().radix_index_select_rows(_ptr(src), src.shape[0], _ptr(_i32(idx, "idx")), n_rows, row_bytes, _ptr(out),
                                         _ptr(status), _stream(stream))
     _check(rc, "radix_index_select_rows")
+    return out
+
+
+# ---- paged key/value cache, attention over it, log-probabilities
+
+_TORCH_DTYPES = {torch.float32: RADIX_F32, torch.bfloat16: RADIX_BF16, torch.float16: RADIX_F16}
+
+
+class _On:
+    """Makes `device` the current one for a call (the library launches on the current device) and yields the stream to use."""
+
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
+        self.guard = torch.cuda.device(device)
+        self.device, self.stream = device, stream
+
+    def __enter__(self) -> int:
+        self.guard.__enter__()
+        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+
+    def __exit__(self, *exc) -> None:
+        self.guard.__exit__(*exc)
+
+
+def _same_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
+
+
+def _list(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
+    """Pointer of an optional int32 list of n entries."""
+    if t is None:
+        return None
+    if _i32(t, name).numel() != n:
+        raise ValueError(f"{name} has {t.numel()} entries, not {n}")
+    return _ptr(t)
+
+
+def _out(t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
+    return t
+
+
+def _status(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else _ptr(_i32(t, "status"))
+
+
+class Cache:
+    """A radix_cache over the caller's tensors: pages [n_layers, n_pages, 2, n_kv_heads, page_size, head_dim] (fp32, bf16 or fp16),
+    page_refs [n_pages], page_table [max_seqs, max_pages] and seq_lens [max_seqs] (int32), as described in radixmlp.h."""
+
+    def __init__(self, pages: torch.Tensor, page_refs: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor):
+        if pages.dim() != 6 or pages.shape[2] != 2 or pages.dtype not in _TORCH_DTYPES or not pages.is_cuda or not pages.is_contiguous():
+            raise TypeError("pages must be a contiguous CUDA tensor [n_layers, n_pages, 2, n_kv_heads, page_size, head_dim] of fp32, bf16 or fp16")
+        _same_device(pages.device, page_refs=page_refs, page_table=page_table, seq_lens=seq_lens)
+        L, n_pages, _, kv, page_size, hd = pages.shape
+        if _i32(page_refs, "page_refs").shape != (n_pages,):
+            raise ValueError(f"page_refs must have shape ({n_pages},)")
+        if _i32(page_table, "page_table").dim() != 2 or _i32(seq_lens, "seq_lens").shape != (page_table.shape[0],):
+            raise ValueError("page_table must be [max_seqs, max_pages] and seq_lens [max_seqs]")
+        self.pages, self.page_refs, self.page_table, self.seq_lens = pages, page_refs, page_table, seq_lens
+        self.device, self.dtype = pages.device, pages.dtype
+        self.n_kv_heads, self.head_dim = kv, hd
+        self.struct = radix_cache(L, kv, hd, page_size, n_pages, _TORCH_DTYPES[pages.dtype], page_table.shape[0], page_table.shape[1],
+                                  _ptr(pages), _ptr(page_refs), _ptr(page_table), _ptr(seq_lens))
+        n = C.c_size_t()
+        _check(_lib().radix_cache_bytes(C.byref(self.struct), C.byref(n)), "radix_cache_bytes")
+        assert n.value == pages.numel() * pages.element_size()
+
+
+def alloc_cache(n_layers: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: torch.dtype, max_seqs: int,
+                max_pages: int, device: str = "cuda") -> Cache:
+    """An empty cache in new tensors."""
+    ints = dict(dtype=torch.int32, device=device)
+    return Cache(torch.empty((n_layers, n_pages, 2, n_kv_heads, page_size, head_dim), dtype=dtype, device=device),
+                 torch.zeros(n_pages, **ints), torch.full((max_seqs, max_pages), -1, **ints), torch.zeros(max_seqs, **ints))
+
+
+def radix_cache_workspace_bytes(cache: Cache, max_n: int) -> int:
+    n = C.c_size_t()
+    _check(_lib().radix_cache_workspace_bytes(C.byref(cache.struct), max_n, C.byref(n)), "radix_cache_workspace_bytes")
+    return n.value
+
+
+def radix_cache_reset(cache: Cache, stream: Optional[torch.cuda.Stream] = None) -> None:
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_reset(C.byref(cache.struct), s), "radix_cache_reset")
+
+
+def radix_cache_extend(cache: Cache, cu_seqlens: torch.Tensor, ws: torch.Tensor, slots: Optional[torch.Tensor] = None,
+                       past: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Room for the batch's new tokens; returns past[B], the lengths before (-1 everywhere if the call was refused)."""
+    B = _i32(cu_seqlens, "cu_seqlens").numel() - 1
+    _same_device(cache.device, cu_seqlens=cu_seqlens, ws=ws, slots=slots, past=past, status=status)
+    past = _out(past, "past", (B,), torch.int32, cache.device)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_extend(C.byref(cache.struct), _list(slots, "slots", B), _ptr(cu_seqlens), B, _ptr(past), _ptr(ws),
+                                         ws.numel(), _status(status), s), "radix_cache_extend")
+    return past
+
+
+def radix_cache_fork(cache: Cache, parents: torch.Tensor, children: torch.Tensor, ws: torch.Tensor,
+                     status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    n = _i32(parents, "parents").numel()
+    _same_device(cache.device, parents=parents, children=children, ws=ws, status=status)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_fork(C.byref(cache.struct), _ptr(parents), _list(children, "children", n), n, _ptr(ws), ws.numel(),
+                                       _status(status), s), "radix_cache_fork")
+
+
+def radix_cache_free(cache: Cache, slots: torch.Tensor, keep_lens: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    n = _i32(slots, "slots").numel()
+    _same_device(cache.device, slots=slots, keep_lens=keep_lens, status=status)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_free(C.byref(cache.struct), _ptr(slots), _list(keep_lens, "keep_lens", n), n, _status(status), s),
+               "radix_cache_free")
+
+
+def radix_cache_compact(cache: Cache, ws: torch.Tensor, n_used: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Returns n_used[1]: used pages, which are pages 0 .. n_used - 1 now."""
+    _same_device(cache.device, ws=ws, n_used=n_used, status=status)
+    n_used = _out(n_used, "n_used", (1,), torch.int32, cache.device)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_compact(C.byref(cache.struct), _ptr(n_used), _ptr(ws), ws.numel(), _status(status), s),
+               "radix_cache_compact")
+    return n_used
+
+
+def radix_cache_copy_pages(cache: Cache, src: torch.Tensor, dst: torch.Tensor, ws: torch.Tensor, status: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> None:
+    n = _i32(src, "src").numel()
+    _same_device(cache.device, src=src, dst=dst, ws=ws, status=status)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_copy_pages(C.byref(cache.struct), _ptr(src), _list(dst, "dst", n), n, _ptr(ws), ws.numel(),
+                                             _status(status), s), "radix_cache_copy_pages")
+
+
+def _token_rows(t: torch.Tensor, name: str, cache: Cache, heads: Optional[int] = None) -> int:
+    """Checks a [N, heads, head_dim] tensor whose tokens are contiguous; returns the elements between tokens."""
+    if t.dim() != 3 or t.dtype != cache.dtype or not t.is_cuda or t.shape[2] != cache.head_dim or (heads and t.shape[1] != heads):
+        raise TypeError(f"{name} must be a CUDA tensor [N, heads, {cache.head_dim}] of the cache's dtype {cache.dtype}")
+    if (t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise TypeError(f"{name}: the heads of a token must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def radix_cache_append(cache: Cache, layer: int, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, past: torch.Tensor,
+                       slots: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """k, v: [N, n_kv_heads, head_dim], may be views into fused q|k|v rows."""
+    B, N = _i32(cu_seqlens, "cu_seqlens").numel() - 1, k.shape[0]
+    if v.shape != k.shape:
+        raise ValueError("k and v differ in shape")
+    ks, vs = _token_rows(k, "k", cache, cache.n_kv_heads), _token_rows(v, "v", cache, cache.n_kv_heads)
+    _same_device(cache.device, k=k, v=v, cu_seqlens=cu_seqlens, past=past, slots=slots, status=status)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_cache_append(C.byref(cache.struct), layer, _ptr(k), ks, _ptr(v), vs, _ptr(cu_seqlens), _list(past, "past", B),
+                                         _list(slots, "slots", B), B, N, _status(status), s), "radix_cache_append")
+
+
+def radix_paged_attention_workspace_bytes(cache: Cache, n_q_heads: int, max_N: int, max_B: int, max_new: int) -> int:
+    n = C.c_size_t()
+    _check(_lib().radix_paged_attention_workspace_bytes(C.byref(cache.struct), n_q_heads, max_N, max_B, max_new, C.byref(n)),
+           "radix_paged_attention_workspace_bytes")
+    return n.value
+
+
+def radix_paged_attention(cache: Cache, layer: int, q: torch.Tensor, cu_seqlens: torch.Tensor, past: torch.Tensor, max_new: int,
+                          ws: torch.Tensor, slots: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                          status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """q: [N, n_q_heads, head_dim], may be a view into fused rows; returns out of that shape."""
+    B, N = _i32(cu_seqlens, "cu_seqlens").numel() - 1, q.shape[0]
+    qs = _token_rows(q, "q", cache)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    os_ = _token_rows(out, "out", cache)
+    _same_device(cache.device, q=q, cu_seqlens=cu_seqlens, past=past, ws=ws, slots=slots, out=out, status=status)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_paged_attention(C.byref(cache.struct), layer, _ptr(q), qs, q.shape[1], _ptr(cu_seqlens), _list(past, "past", B),
+                                            _list(slots, "slots", B), B, N, max_new, _ptr(out), os_, _ptr(ws), ws.numel(), _status(status), s),
+               "radix_paged_attention")
+    return out
+
+
+def radix_extend_workspace_bytes(model: Model, cache: Cache, max_N: int, max_B: int, max_new: int) -> int:
+    n = C.c_size_t()
+    _check(_lib().radix_extend_workspace_bytes(model.handle, C.byref(cache.struct), max_N, max_B, max_new, C.byref(n)),
+           "radix_extend_workspace_bytes")
+    return n.value
+
+
+def radix_extend_forward(model: Model, cache: Cache, tok: torch.Tensor, cu_seqlens: torch.Tensor, max_new: int, ws: torch.Tensor,
+                         slots: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Forward of the new tokens tok[N] behind what the cache holds of their slots; returns the hidden states [N, d]."""
+    N, B = _i32(tok, "tok").numel(), _i32(cu_seqlens, "cu_seqlens").numel() - 1
+    _same_device(cache.device, tok=tok, cu_seqlens=cu_seqlens, ws=ws, slots=slots, out=out)
+    out = _out(out, "out", (N, model.cfg.d), torch.float32, cache.device)
+    with _On(cache.device, stream) as s:
+        _check(_lib().radix_extend_forward(model.handle, C.byref(cache.struct), _ptr(tok), _ptr(cu_seqlens), _list(slots, "slots", B), B, N,
+                                           max_new, _ptr(out), _ptr(ws), ws.numel(), s), "radix_extend_forward")
+    return out
+
+
+def radix_token_logprobs_workspace_bytes(max_rows: int, vocab: int, n_given: int, top_k: int) -> int:
+    n = C.c_size_t()
+    _check(_lib().radix_token_logprobs_workspace_bytes(max_rows, vocab, n_given, top_k, C.byref(n)), "radix_token_logprobs_workspace_bytes")
+    return n.value
+
+
+def _given(given: Optional[torch.Tensor], n: int) -> int:
+    if given is None:
+        return 0
+    if _i32(given, "given").dim() != 2 or given.shape[0] != n:
+        raise ValueError(f"given must be [{n}, n_given]")
+    return given.shape[1]
+
+
+def _answers(n: int, n_given: int, top_k: int, dev: torch.device) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    f = dict(dtype=torch.float32, device=dev)
+    return (torch.empty((n, n_given), **f), torch.empty(n, **f), torch.empty((n, top_k), dtype=torch.int32, device=dev),
+            torch.empty((n, top_k), **f))
+
+
+def radix_token_logprobs(logits: torch.Tensor, given: Optional[torch.Tensor], ws: torch.Tensor, top_k: int = 0,
+                         status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                         ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """logits [n, vocab] (rows may be strided), given [n, n_given] int32 or None.  Returns (logprobs [n, n_given], entropy [n],
+    top_ids [n, top_k], top_logprobs [n, top_k])."""
+    if logits.dim() != 2 or logits.dtype not in _TORCH_DTYPES or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError("logits must be a CUDA tensor [n, vocab] of fp32, bf16 or fp16 with contiguous rows")
+    n, vocab = logits.shape
+    g = _given(given, n)
+    _same_device(logits.device, given=given, ws=ws, status=status)
+    out = _answers(n, g, max(top_k, 0), logits.device)
+    with _On(logits.device, stream) as s:
+        _check(_lib().radix_token_logprobs(_ptr(logits), _TORCH_DTYPES[logits.dtype], logits.stride(0) if n > 1 else vocab, n, vocab,
+                                           _ptr(given), g, top_k, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(ws),
+                                           ws.numel(), _status(status), s), "radix_token_logprobs")
+    return out
+
+
+def radix_score_tokens_workspace_bytes(model: Model, max_rows: int, n_given: int, top_k: int) -> int:
+    n = C.c_size_t()
+    _check(_lib().radix_score_tokens_workspace_bytes(model.handle, max_rows, n_given, top_k, C.byref(n)), "radix_score_tokens_workspace_bytes")
+    return n.value
+
+
+def radix_score_tokens(model: Model, hidden: torch.Tensor, rows: Optional[torch.Tensor], given: Optional[torch.Tensor], ws: torch.Tensor,
+                       top_k: int = 0, n_rows: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None
+                       ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """radix_lm_head of hidden[rows] (or of the first n_rows rows) and radix_token_logprobs of its logits, which are not kept."""
+    if hidden.dtype != torch.float32 or not hidden.is_cuda or not hidden.is_contiguous():
+        raise TypeError("hidden must be a contiguous fp32 CUDA tensor")
+    n_src = hidden.shape[0]
+    n = rows.numel() if rows is not None else (n_src if n_rows is None else n_rows)
+    g = _given(given, n)
+    _same_device(hidden.device, rows=rows, given=given, ws=ws)
+    out = _answers(n, g, max(top_k, 0), hidden.device)
+    with _On(hidden.device, stream) as s:
+        _check(_lib().radix_score_tokens(model.handle, _ptr(hidden), n_src, _list(rows, "rows", n), n, _ptr(given), g, top_k, _ptr(out[0]),
+                                         _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(ws), ws.numel(), s), "radix_score_tokens")
     return out
 
 

@@ -12,7 +12,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libradixmlp.so")
 
 SOURCES = ["index_build.hip", "rowops.hip", "gemm_f32.hip", "gemm_mfma.hip", "gemm_small.hip", "attention_f32.hip",
-           "attention_mfma.hip", "model.hip"]
+           "attention_mfma.hip", "cache_pages.hip", "paged_attention.hip", "token_logprobs.hip", "cache_api.hip", "model.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

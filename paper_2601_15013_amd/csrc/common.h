@@ -14,6 +14,7 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 #define RADIX_WAVE 64
 
@@ -24,7 +25,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
     } while (0)
 
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+__host__ __device__ static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -77,4 +78,19 @@ template <> struct Op<RADIX_F16> {
 // Device status word: first error wins.
 __device__ __forceinline__ void set_status(int32_t* status, int32_t code) {
     if (status) atomicCAS(status, 0, code);
+}
+
+// The sequence that token i lies in: the smallest s with cu[s + 1] > i, searched by the whole wavefront, 64 candidates
+// a step (i is the same in all lanes).  Three dependent loads for 65 000 sequences where a search by halves takes 16.
+__device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B, int i, int lane) {
+    int lo = 0, n = B;                                      // the answer is in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 63) >> 6, first = lane * step;
+        const int last = first + step < n ? first + step - 1 : n - 1;       // last candidate of this lane's share
+        const unsigned long long past = __ballot(cu[lo + last + 1] > i);
+        const int f = past ? __ffsll((long long)past) - 1 : (n - 1) / step;
+        lo += f * step;
+        n = n - f * step < step ? n - f * step : step;
+    }
+    return lo;
 }

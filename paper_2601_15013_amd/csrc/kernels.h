@@ -41,6 +41,9 @@ void launch_rows_to_operand(const float* src, int n_src, const int32_t* sel, int
 // dst[i] = (f16) src[i] for n bf16 values (weights handed over as bf16, multiplied as fp16)
 void launch_bf16_to_f16(const bf16_t* src, f16_t* dst, size_t n, hipStream_t stream);
 
+// pos[i] = past[b] + i - cu[b] for token i of sequence b (past[b] < 0: 0)
+void launch_paged_positions(const int32_t* cu, const int32_t* past, int B, int N, int32_t* pos, hipStream_t stream);
+
 // ---- GEMMs: C[M, Nout] = A[M, K] * W[Nout, K]^T with an epilogue
 enum GemmEpilogue {
     EPI_STORE = 0,     // C stored in the activation dtype
@@ -212,3 +215,80 @@ static inline AttnPlanLayout attn_plan_layout(size_t N, size_t B) {
 }
 void launch_attn_plan(const int32_t* cu, const int32_t* I_scatter, const int32_t* I_gather, int B, int N,
                       int n_compact, int n_q_heads, int n_kv_heads, int32_t* plan, hipStream_t stream);
+
+// ---- paged key/value cache (cache_pages.hip, paged_attention.hip)
+// What the kernels see of a radix_cache.  A piece is one head's keys (or values) of a page; a page of a layer is
+// n_kv_heads pieces of keys, then n_kv_heads pieces of values.
+struct CacheView {
+    char* pages;
+    int32_t *refs, *table, *lens;
+    int n_layers, n_pages, n_kv_heads, head_dim, page_size, page_shift, max_seqs, max_pages;     // page_size = 1 << page_shift
+    size_t piece_bytes, page_bytes, layer_bytes;
+};
+// Scratch of the page calls, in int32 words behind a header {number of moves, ...} of 64 words.
+struct PageWs {
+    uint32_t mark, map, list, src, dst, rows, first, shared;
+    size_t total;                        // below 2^32
+};
+static inline PageWs page_ws_layout(size_t max_seqs, size_t n_pages, size_t n) {
+    PageWs L;
+    size_t off = 64;
+    const size_t moves = n > n_pages ? n : n_pages;
+    auto take = [&](size_t words) { const size_t o = off; off += words; return (uint32_t)o; };
+    L.mark = take(max_seqs);
+    L.map = take(n_pages);
+    L.list = take(n_pages);
+    L.src = take(moves);
+    L.dst = take(moves);
+    L.rows = take(moves);
+    L.first = take(n + 1);
+    L.shared = take(n);
+    L.total = off;
+    return L;
+}
+void launch_cache_reset(const CacheView& c, hipStream_t stream);
+// limit: most tokens a sequence may hold (<= max_pages * page_size)
+// gate: nothing is done where *gate holds an error already (nullptr: no gate)
+void launch_cache_extend(const CacheView& c, const int32_t* slots, const int32_t* cu, int B, int limit, int32_t* past, int32_t* ws,
+                         const int32_t* gate, int32_t* status, hipStream_t stream);
+void launch_cache_fork(const CacheView& c, const int32_t* parents, const int32_t* children, int n, int32_t* ws, int32_t* status,
+                       hipStream_t stream);
+void launch_cache_free(const CacheView& c, const int32_t* slots, const int32_t* keep, int n, int32_t* status, hipStream_t stream);
+void launch_cache_compact(const CacheView& c, int32_t* n_used, int32_t* ws, int32_t* status, hipStream_t stream);
+void launch_cache_copy(const CacheView& c, const int32_t* src, const int32_t* dst, int n, int32_t* ws, int32_t* status,
+                       hipStream_t stream);
+// k, v: rows of n_kv_heads * head_dim values, k_stride / v_stride bytes apart
+void launch_cache_append(const CacheView& c, int layer, const void* k, const void* v, size_t k_stride, size_t v_stride,
+                         const int32_t* cu, const int32_t* past, const int32_t* slots, int B, int N, int32_t* status,
+                         hipStream_t stream);
+
+// Attention of new tokens over the cache.  Sequence b has n = cu[b + 1] - cu[b] new tokens behind past[b] cached ones; its
+// rows - (token, query head of the group) pairs of one kv head, token-major - are cut into blocks.  Sequences of up to
+// `few_rows` rows are walked by the kernel for few rows (and all of them with fp32), the others by the kernel for many.  A block's
+// keys are split over several workgroups where the batch has too few blocks for the chip; their results are joined afterwards.
+// plan[] (int32): {split length of the few kernel in its tiles, of the many kernel}, then prefix sums over the sequences: items of
+// either kernel, units of the join (blocks that are split), partial results of either kernel; the number of splits.
+struct PagedShape {
+    int n_q_heads, B, N, max_new;
+    size_t q_stride, out_stride;         // elements between tokens
+};
+struct PagedLayout {
+    size_t item_few, item_many, unit, slot_few, slot_many, splits, total_words;  // int32 words
+    size_t few_acc, few_ml, many_acc, many_ml, total;                            // bytes
+    int few_rows, few_tile, many;        // rows of a block / keys of a tile of the few kernel; whether the many kernel can have work
+    long long few_items, many_items, few_slots, many_slots, units;               // upper bounds
+};
+PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s);
+// plan: the lists above (words of `ws`), and the check of cu, past and slots: a sequence that fails it gets zeros (or nothing, if its
+// rows are not in [0, N)) and is reported in *status.
+void launch_paged_plan(const CacheView& c, const PagedShape& s, const PagedLayout& L, const int32_t* cu, const int32_t* past,
+                       const int32_t* slots, void* ws, int32_t* status, hipStream_t stream);
+int launch_paged_attention(const CacheView& c, int dtype, int layer, const PagedShape& s, const PagedLayout& L, const void* q,
+                           const int32_t* cu, const int32_t* past, const int32_t* slots, void* out, void* ws, int32_t* status,
+                           hipStream_t stream);
+
+// ---- log-probabilities (token_logprobs.hip): logits [n_rows, vocab] of `dtype`, rows ld elements apart; k <= 32
+size_t token_logprobs_ws_bytes(int n_rows, int k);
+void launch_token_logprobs(const void* logits, int dtype, size_t ld, int n_rows, int vocab, const int32_t* given, int n_given, int k,
+                           float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs, void* ws, int32_t* status,
+                           hipStream_t stream);

@@ -4,6 +4,7 @@
 #include <new>
 #include <vector>
 
+#include "cache_view.h"
 #include "common.h"
 #include "kernels.h"
 #include "radixmlp_bench.h"
@@ -309,9 +310,20 @@ extern "C" int radix_device_status(void* ws, size_t ws_bytes, void* stream) {
 
 namespace {
 
+// A forward over a cache: the cache, the new tokens' places in it and the attention's plan.
+struct PagedRun {
+    CacheView cache;
+    PagedShape shape;
+    PagedLayout layout;
+    const int32_t *slots, *pos;
+    int32_t* past;
+    void *page_ws, *attn_ws;
+    int limit;                       // most positions of a sequence
+};
+
 int forward_impl(const radix_model* model, const int32_t* tok, const int32_t* pos, const int32_t* cu, int B, int N,
                  int max_seqlen, const int32_t* Is, const int32_t* Ig, int M, bool dedup, bool fused, int pad_to,
-                 float* out, void* ws, size_t ws_bytes, hipStream_t stream) {
+                 float* out, void* ws, size_t ws_bytes, hipStream_t stream, const PagedRun* paged = nullptr) {
     const radix_model_config& c = model->cfg;
     const bool direct = fused && dedup && c.compute_dtype == RADIX_F32;      // fp32: the attention kernel reads through the maps
     fused = fused && dedup && !direct;
@@ -330,6 +342,12 @@ int forward_impl(const radix_model* model, const int32_t* tok, const int32_t* po
         return RADIX_OK;
     }
     launch_validate_cu(cu, B, N, max_seqlen, hdr, stream);
+    if (paged) {
+        launch_cache_extend(paged->cache, paged->slots, cu, B, paged->limit, paged->past, (int32_t*)paged->page_ws, hdr, hdr, stream);
+        launch_paged_positions(cu, paged->past, B, N, const_cast<int32_t*>(paged->pos), stream);
+        launch_paged_plan(paged->cache, paged->shape, paged->layout, cu, paged->past, paged->slots, paged->attn_ws, hdr, stream);
+        pos = paged->pos;
+    }
 
     const int dt = c.compute_dtype;          // activation / operand type
     const size_t es = esize(dt);
@@ -402,7 +420,7 @@ int forward_impl(const radix_model* model, const int32_t* tok, const int32_t* po
         // Q/K-norm and RoPE ride in the QKV GEMM's epilogue when a wavefront block is one head; in a (hi, lo) layer
         // that epilogue also writes q, k and v as (hi, lo) pairs, which attention then multiplies term by term
         const bool fused_rope = dt != RADIX_F32 && hd == 128 && row % 256 == 0;
-        const bool qkv_split = hl && fused_rope;
+        const bool qkv_split = hl && fused_rope && !paged;       // (a cache holds single values)
         const int q2 = qkv_split ? 2 : 1;
         {
             TimedScope t(t_qkv, stream);
@@ -417,7 +435,17 @@ int forward_impl(const radix_model* model, const int32_t* tok, const int32_t* po
             launch_qknorm_rope(qkv, dt, M, c.n_q_heads, c.n_kv_heads, hd, c.qk_norm, Lw.gq, Lw.gk, c.eps, pos_c,
                                model->cos_tab, model->sin_tab, stream);
         }
-        const size_t attn_row_bytes = (size_t)w2 * dq * es;
+        const int a2 = paged ? 1 : w2;
+        const size_t attn_row_bytes = (size_t)a2 * dq * es;
+        if (paged) {       // new keys and values into the cache, then attention over it
+            TimedScope t(RADIX_TIME_ATTENTION, stream);
+            const char* k = (const char*)qkv + (size_t)dq * es;
+            launch_cache_append(paged->cache, l, k, k + (size_t)dkv * es, (size_t)row * es, (size_t)row * es, cu, paged->past, paged->slots, B,
+                                N, hdr, stream);
+            rc = launch_paged_attention(paged->cache, dt, l, paged->shape, paged->layout, qkv, cu, paged->past, paged->slots, attn_c,
+                                        paged->attn_ws, hdr, stream);
+            if (rc != RADIX_OK) return rc;
+        }
         if (fused) {   // scatter, attention and gather in one kernel (exact): compact rows in, compact rows out
             TimedScope t(RADIX_TIME_ATTENTION, stream);
             rc = launch_attention_mfma_fused(qkv, cu, Is, plan, B, N, M_valid, c.n_q_heads, c.n_kv_heads, hd, attn_c,
@@ -431,7 +459,7 @@ int forward_impl(const radix_model* model, const int32_t* tok, const int32_t* po
             TimedScope t(RADIX_TIME_SCATTER, stream);
             launch_index_select_rows(qkv, M_valid, Is, N, (size_t)q2 * row * es, qkv_full, hdr, stream);
         }
-        if (!fused) {
+        if (!fused && !paged) {
             TimedScope t(RADIX_TIME_ATTENTION, stream);
             if (dt != RADIX_F32) {
                 rc = launch_attention_mfma(qkv_full, cu, B, N, max_seqlen, c.n_q_heads, c.n_kv_heads, hd, attn_full,
@@ -457,7 +485,7 @@ int forward_impl(const radix_model* model, const int32_t* tok, const int32_t* po
             const bool fold2 = can_fold && !hl;     // this projection prepares the post-attention norm
             NormFusion produce = {};
             produce.a16 = a; produce.gain = Lw.g2; produce.ss_out = ss;
-            rc = gemm(gather_in_gemm ? attn_full : attn_c, Lw.wo, d, w2 * dq, dq, fold2 ? EPI_RESIDUAL_NORM : EPI_RESIDUAL, h,
+            rc = gemm(gather_in_gemm ? attn_full : attn_c, Lw.wo, d, a2 * dq, dq, fold2 ? EPI_RESIDUAL_NORM : EPI_RESIDUAL, h,
                       nullptr, gather_in_gemm ? &amap : nullptr, fold2 ? &produce : nullptr);
             if (rc != RADIX_OK) return rc;
             normed = fold2;
@@ -594,6 +622,72 @@ extern "C" int radix_prefill_forward_nodedup(const radix_model* model, const int
                         ws_bytes, (hipStream_t)stream);
 }
 
+namespace {
+
+// Workspace of radix_extend_forward: the forward's, then what the cache's calls need.
+struct ExtendWs { size_t past, pos, page, attn, total; };
+int extend_setup(const radix_model* model, const radix_cache* cache, int N, int B, int max_new, CacheView* v, PagedShape* s, PagedLayout* P,
+                 ExtendWs* L) {
+    const radix_model_config& c = model->cfg;
+    const int rc = cache_shape(cache, v);
+    if (rc != RADIX_OK) return rc;
+    if (cache->n_layers != c.n_layers || cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim || cache->dtype != c.compute_dtype)
+        return RADIX_ERR_BAD_CONFIG;
+    if (N < 0 || B < 0 || max_new < 0) return RADIX_ERR_BAD_SIZE;
+    if (B > RADIX_CACHE_MAX_LIST || (int64_t)N * c.n_q_heads > INT32_MAX || (int64_t)B * c.n_q_heads > INT32_MAX / 4) return RADIX_ERR_UNSUPPORTED;
+    const size_t hd = c.head_dim, row = (c.n_q_heads + 2 * (size_t)c.n_kv_heads) * hd;
+    *s = {c.n_q_heads, B, N, max_new < N ? max_new : N, row, c.n_q_heads * hd};
+    *P = paged_layout(*v, cache->dtype, *s);
+    if (P->few_items > INT32_MAX || P->many_items > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
+    size_t off = align_up(ws_layout(c, model->hilo_layers, (size_t)N, (size_t)B).total, 256);
+    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes ? bytes : 1, 256); return o; };
+    L->past = take((size_t)B * 4);
+    L->pos = take((size_t)N * 4);
+    L->page = take(page_ws_layout(v->max_seqs, v->n_pages, (size_t)B).total * 4);
+    L->attn = take(P->total);
+    L->total = off;
+    return RADIX_OK;
+}
+
+}  // namespace
+
+extern "C" int radix_extend_workspace_bytes(const radix_model* model, const radix_cache* cache, int32_t max_N, int32_t max_B, int32_t max_new,
+                                            size_t* bytes_out) {
+    if (!model || !cache || !bytes_out) return RADIX_ERR_NULL_POINTER;
+    CacheView v;
+    PagedShape s;
+    PagedLayout P;
+    ExtendWs L;
+    const int rc = extend_setup(model, cache, max_N, max_B, max_new, &v, &s, &P, &L);
+    if (rc != RADIX_OK) return rc;
+    *bytes_out = L.total;
+    return RADIX_OK;
+}
+
+extern "C" int radix_extend_forward(const radix_model* model, const radix_cache* cache, const int32_t* tok, const int32_t* cu_seqlens,
+                                    const int32_t* slots, int32_t B, int32_t N, int32_t max_new, float* out, void* ws, size_t ws_bytes,
+                                    void* stream) {
+    int rc = check_common(model, tok, cu_seqlens, B, N, max_new, out, ws);
+    if (rc != RADIX_OK) return rc;
+    PagedRun run;
+    ExtendWs L;
+    rc = extend_setup(model, cache, N, B, max_new, &run.cache, &run.shape, &run.layout, &L);
+    if (rc == RADIX_OK) rc = cache_view(cache, &run.cache);
+    if (rc != RADIX_OK) return rc;
+    if (!slots && B > run.cache.max_seqs) return RADIX_ERR_BAD_SIZE;
+    if (ws_bytes < L.total) return RADIX_ERR_WORKSPACE_TOO_SMALL;
+    char* w = (char*)ws;
+    run.slots = slots;
+    run.past = (int32_t*)(w + L.past);
+    run.pos = (const int32_t*)(w + L.pos);
+    run.page_ws = w + L.page;
+    run.attn_ws = w + L.attn;
+    const int64_t room = (int64_t)run.cache.max_pages * run.cache.page_size;
+    run.limit = room < model->cfg.max_pos ? (int)room : model->cfg.max_pos;
+    return forward_impl(model, tok, nullptr, cu_seqlens, B, N, max_new, nullptr, nullptr, N, false, false, 0, out, ws, ws_bytes,
+                        (hipStream_t)stream, &run);
+}
+
 extern "C" int radix_lm_head_workspace_bytes(const radix_model* model, int32_t max_rows, size_t* bytes_out) {
     if (!model || !bytes_out) return RADIX_ERR_NULL_POINTER;
     if (max_rows < 0) return RADIX_ERR_BAD_SIZE;
@@ -626,6 +720,62 @@ extern "C" int radix_lm_head(const radix_model* model, const float* hidden, int3
     } else {
         const int rc = launch_gemm_mfma(a, model->lm_head, n_rows, c.vocab, c.d, EPI_STORE_F32, logits, dt, 0, stream);
         if (rc != RADIX_OK) return rc;
+    }
+    HIP_TRY(hipGetLastError());
+    return RADIX_OK;
+}
+
+extern "C" int radix_score_tokens_workspace_bytes(const radix_model* model, int32_t max_rows, int32_t n_given, int32_t top_k,
+                                                  size_t* bytes_out) {
+    if (!model || !bytes_out) return RADIX_ERR_NULL_POINTER;
+    if (max_rows < 0) return RADIX_ERR_BAD_SIZE;
+    const int rows = max_rows < RADIX_SCORE_ROWS ? max_rows : RADIX_SCORE_ROWS;
+    size_t head = 0, probs = 0;
+    int rc = radix_lm_head_workspace_bytes(model, rows, &head);
+    if (rc == RADIX_OK) rc = radix_token_logprobs_workspace_bytes(rows, model->cfg.vocab, n_given, top_k, &probs);
+    if (rc != RADIX_OK) return rc;
+    *bytes_out = head + align_up((size_t)rows * model->cfg.vocab * 4, 256) + probs;
+    return RADIX_OK;
+}
+
+extern "C" int radix_score_tokens(const radix_model* model, const float* hidden, int32_t n_src_rows, const int32_t* rows, int32_t n_rows,
+                                  const int32_t* given, int32_t n_given, int32_t top_k, float* logprobs, float* entropy, int32_t* top_ids,
+                                  float* top_logprobs, void* ws, size_t ws_bytes, void* stream_) {
+    if (!model || !ws) return RADIX_ERR_NULL_POINTER;
+    if (n_src_rows < 0 || n_rows < 0) return RADIX_ERR_BAD_SIZE;
+    if (!rows && n_rows > n_src_rows) return RADIX_ERR_BAD_SIZE;
+    if (!model->lm_head) return RADIX_ERR_UNSUPPORTED;
+    const radix_model_config& c = model->cfg;
+    size_t need = 0, head = 0, probs = 0;
+    const int rc = radix_score_tokens_workspace_bytes(model, n_rows, n_given, top_k, &need);
+    if (rc != RADIX_OK) return rc;
+    if (ws_bytes < need) return RADIX_ERR_WORKSPACE_TOO_SMALL;
+    if ((((uintptr_t)ws) & 255) != 0) return RADIX_ERR_MISALIGNED;
+    hipStream_t stream = (hipStream_t)stream_;
+    int32_t* hdr = (int32_t*)ws;
+    if (n_rows > 0 && (!hidden || (n_given > 0 && (!given || !logprobs)) || (top_k > 0 && (!top_ids || !top_logprobs)))) return RADIX_ERR_NULL_POINTER;
+    if (n_rows > 0 && n_src_rows == 0) return RADIX_ERR_BAD_SIZE;
+    hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, stream, hdr);
+    const int most = n_rows < RADIX_SCORE_ROWS ? n_rows : RADIX_SCORE_ROWS;
+    radix_lm_head_workspace_bytes(model, most, &head);
+    radix_token_logprobs_workspace_bytes(most, c.vocab, n_given, top_k, &probs);
+    void* a = (char*)ws + RADIX_WS_HEADER_BYTES;
+    float* logits = (float*)((char*)ws + head);
+    void* pw = (char*)logits + align_up((size_t)most * c.vocab * 4, 256);
+    const int dt = c.compute_dtype;
+    for (int r0 = 0; r0 < n_rows; r0 += RADIX_SCORE_ROWS) {
+        const int n = n_rows - r0 < RADIX_SCORE_ROWS ? n_rows - r0 : RADIX_SCORE_ROWS;
+        if (rows) launch_rows_to_operand(hidden, n_src_rows, rows + r0, n, c.d, a, dt, hdr, stream);
+        else launch_rows_to_operand(hidden + (size_t)r0 * c.d, n_src_rows - r0, nullptr, n, c.d, a, dt, hdr, stream);
+        if (dt == RADIX_F32) {
+            launch_gemm_f32((const float*)a, (const float*)model->lm_head, n, c.vocab, c.d, EPI_STORE, logits, stream);
+        } else {
+            const int grc = launch_gemm_mfma(a, model->lm_head, n, c.vocab, c.d, EPI_STORE_F32, logits, dt, 0, stream);
+            if (grc != RADIX_OK) return grc;
+        }
+        launch_token_logprobs(logits, RADIX_F32, (size_t)c.vocab, n, c.vocab, n_given ? given + (size_t)r0 * n_given : nullptr, n_given, top_k,
+                              n_given ? logprobs + (size_t)r0 * n_given : nullptr, entropy ? entropy + r0 : nullptr,
+                              top_k ? top_ids + (size_t)r0 * top_k : nullptr, top_k ? top_logprobs + (size_t)r0 * top_k : nullptr, pw, hdr, stream);
     }
     HIP_TRY(hipGetLastError());
     return RADIX_OK;
@@ -668,6 +818,9 @@ extern "C" const char* radix_status_string(int status) {
         case RADIX_ERR_HIP: return "HIP runtime error";
         case RADIX_ERR_BAD_CONFIG: return "inconsistent model configuration";
         case RADIX_ERR_STATIC_LIMIT: return "more sequences than the static scratch array of radix_build_index_static holds";
+        case RADIX_ERR_BAD_PAGE: return "a cache position without a page, or a page id out of range or listed twice";
+        case RADIX_ERR_OUT_OF_PAGES: return "no free page left, or a sequence longer than its row of the page table";
+        case RADIX_ERR_BAD_SLOT: return "cache slot out of range, listed twice or not empty";
         default: return "unknown status";
     }
 }

@@ -62,21 +62,6 @@ __global__ __launch_bounds__(1024) void validate_cu_kernel(const int32_t* __rest
     if (bad) set_status(status, RADIX_ERR_BAD_CU_SEQLENS);
 }
 
-// The sequence that token i lies in: the smallest s with cu[s + 1] > i, searched by the whole wavefront, 64 candidates
-// a step (i is the same in all lanes).  Three dependent loads for 65 000 sequences where a search by halves takes 16.
-__device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B, int i, int lane) {
-    int lo = 0, n = B;                                      // the answer is in [lo, lo + n)
-    while (n > 1) {
-        const int step = (n + 63) >> 6, first = lane * step;
-        const int last = first + step < n ? first + step - 1 : n - 1;       // last candidate of this lane's share
-        const unsigned long long past = __ballot(cu[lo + last + 1] > i);
-        const int f = past ? __ffsll((long long)past) - 1 : (n - 1) / step;
-        lo += f * step;
-        n = n - f * step < step ? n - f * step : step;
-    }
-    return lo;
-}
-
 // One wavefront per compact row: which token it represents, its position id (pos == nullptr: its offset in its
 // sequence) and its embedding as fp32.  Latency-bound for small batches, so the steps share one launch (with
 // the clearing and the check of cu_seqlens in another, a forward starts with two launches instead of five: the call of

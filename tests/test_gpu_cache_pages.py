@@ -1,0 +1,284 @@
+"""Pages of a cache on the GPU against a pool of Python lists: which page goes where is exact, and so are the copied contents."""
+import random
+
+import pytest
+import torch
+
+from paper_2601_15013_amd import binding
+from tests import cache_util as CU
+
+pytestmark = pytest.mark.gpu
+
+BAD_CU, BAD_PAGE, OUT_OF_PAGES, BAD_SLOT = -6, -11, -12, -13
+
+
+def make(n_pages, page, max_seqs, max_pages, layers=2, kv=2, hd=128, dtype="bf16"):
+    cache = binding.alloc_cache(layers, kv, hd, page, n_pages, CU.DT[dtype], max_seqs, max_pages)
+    cache.pages.copy_(torch.randn(cache.pages.shape, device="cuda"))
+    ws = binding.alloc_workspace(binding.radix_cache_workspace_bytes(cache, 256))
+    ws.fill_(0x5A)                                        # nothing in a workspace may be relied on
+    return cache, CU.Pool(n_pages, page, max_seqs, max_pages), ws, cache.pages.cpu().clone()
+
+
+def extend(cache, pool, ws, slots, news, pages=None):
+    past = binding.radix_cache_extend(cache, CU.i32(CU.ragged(news)), ws, slots=CU.i32(slots))
+    assert past.tolist() == pool.extend(slots, news, pages)
+    pool.agrees(cache)
+
+
+@pytest.mark.parametrize("page,dtype,hd,kv", [(16, "bf16", 128, 2), (64, "f16", 128, 1), (32, "f32", 80, 3), (256, "f32", 4, 1)])
+def test_a_life_of_random_calls(page, dtype, hd, kv):
+    cache, pool, ws, pages = make(150, page, 24, 6, kv=kv, hd=hd, dtype=dtype)
+    status = CU.status_word()
+    rng = random.Random(page)
+    for step in range(60):
+        what = rng.choice(["extend", "extend", "fork", "free", "cut", "compact"])
+        live = [s for s in range(24) if pool.lens[s] > 0]
+        empty = [s for s in range(24) if pool.lens[s] == 0]
+        if what == "extend":
+            slots = rng.sample(range(24), rng.randint(1, 8))
+            news = [rng.choice([0, 1, 1, 5, page, 2 * page - 3]) for _ in slots]
+            news = [min(n, 6 * page - pool.lens[s]) for s, n in zip(slots, news)]
+            if sum(-(-n // page) + 2 for n in news) > pool.refs.count(0):
+                continue
+            past = binding.radix_cache_extend(cache, CU.i32(CU.ragged(news)), ws, slots=CU.i32(slots), status=status)
+            assert past.tolist() == pool.extend(slots, news, pages)
+        elif what == "fork" and live and empty and pool.refs.count(0) > 8:
+            kids = rng.sample(empty, min(len(empty), rng.randint(1, 6)))
+            parents = [rng.choice(live) for _ in kids]
+            binding.radix_cache_fork(cache, CU.i32(parents), CU.i32(kids), ws, status=status)
+            pool.fork(parents, kids, pages)
+        elif what == "free" and len(live) > 2:
+            slots = rng.sample(live, 2)
+            binding.radix_cache_free(cache, CU.i32(slots), status=status)
+            pool.free(slots)
+        elif what == "cut" and live:
+            slots = rng.sample(live, min(len(live), 3))
+            keep = [rng.randint(0, pool.lens[s] + 2) for s in slots]
+            binding.radix_cache_free(cache, CU.i32(slots), keep_lens=CU.i32(keep), status=status)
+            pool.free(slots, keep)
+        elif what == "compact":
+            used = binding.radix_cache_compact(cache, ws, status=status)
+            assert int(used) == pool.compact(pages)
+        pool.agrees(cache)
+        assert torch.equal(cache.pages.cpu(), pages), f"contents differ after step {step} ({what})"
+    assert int(status) == 0
+
+
+def test_a_shortened_fork_gets_a_page_of_its_own_before_it_grows():
+    cache, pool, ws, pages = make(20, 16, 6, 4)
+    extend(cache, pool, ws, [0], [40])                                       # pages 0, 1, and 2 with 8 rows
+    binding.radix_cache_fork(cache, CU.i32([0, 0]), CU.i32([3, 4]), ws)
+    pool.fork([0, 0], [3, 4], pages)
+    binding.radix_cache_free(cache, CU.i32([3, 4]), keep_lens=CU.i32([21, 21]))
+    pool.free([3, 4], [21, 21])
+    pool.agrees(cache)
+    extend(cache, pool, ws, [3, 4, 0], [1, 0, 1], pages)                     # 3 leaves page 1, 4 takes nothing and stays, 0 has its own
+    assert pool.table[3][1] != pool.table[0][1] == pool.table[4][1]
+    extend(cache, pool, ws, [4], [20], pages)
+    assert torch.equal(cache.pages.cpu(), pages)
+
+
+@pytest.mark.parametrize("n_pages", [1, 63, 64, 4095, 4096, 4097, 9001])
+def test_pages_are_found_wherever_they_are(n_pages):
+    cache, pool, ws, _ = make(n_pages, 16, 3, 9001, layers=1, kv=1)
+    extend(cache, pool, ws, [1], [16 * n_pages])                             # the whole pool
+    binding.radix_cache_free(cache, CU.i32([1]))
+    pool.free([1])
+    refs = [1] * n_pages
+    for p in {0, n_pages // 2, n_pages - 1}:
+        refs[p] = 0
+    cache.page_refs.copy_(CU.i32(refs))
+    pool.refs = list(refs)
+    extend(cache, pool, ws, [2, 0], [1, 16 * (refs.count(0) - 1)])
+
+
+def test_many_sequences_and_more_than_a_workgroup_of_entries():
+    n = 2500
+    cache = binding.alloc_cache(1, 1, 128, 16, 3 * n, torch.float16, n, 4)
+    pool = CU.Pool(3 * n, 16, n, 4)
+    ws = binding.alloc_workspace(binding.radix_cache_workspace_bytes(cache, n))
+    rng = random.Random(3)
+    slots = rng.sample(range(n), n)
+    extend(cache, pool, ws, slots, [rng.randint(0, 40) for _ in slots])
+    slots = rng.sample(range(n), n)
+    gone = slots[:n // 2]
+    binding.radix_cache_free(cache, CU.i32(gone))
+    pool.free(gone)
+    pool.agrees(cache)
+    assert int(binding.radix_cache_compact(cache, ws)) == pool.compact()
+    pool.agrees(cache)
+    extend(cache, pool, ws, slots, [rng.randint(0, 5) for _ in slots])
+
+
+@pytest.mark.parametrize("what", ["extend", "fork"])
+def test_an_exhausted_pool_changes_nothing(what):
+    cache, pool, ws, pages = make(8, 16, 6, 8)
+    extend(cache, pool, ws, [0, 1], [40, 60])                                # 3 + 4 pages, one left
+    status = CU.status_word()
+    if what == "extend":
+        past = binding.radix_cache_extend(cache, CU.i32([0, 9, 30]), ws, slots=CU.i32([0, 3]), status=status)
+        assert past.tolist() == [-1, -1]
+    else:
+        binding.radix_cache_fork(cache, CU.i32([0, 1]), CU.i32([2, 3]), ws, status=status)
+    assert int(status) == OUT_OF_PAGES
+    pool.agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+    extend(cache, pool, ws, [3], [16])                                       # the last page can still be had
+    status.zero_()
+    past = binding.radix_cache_extend(cache, CU.i32([0, 1]), ws, slots=CU.i32([1]), past=CU.i32([7]), status=status)      # room in its page
+    assert past.tolist() == pool.extend([1], [1]) and int(status) == 0
+
+
+@pytest.mark.parametrize("slots,cu,code", [([0, 0], [0, 1, 2], BAD_SLOT), ([0, 6], [0, 1, 2], BAD_SLOT), ([-1, 0], [0, 1, 2], BAD_SLOT),
+                                           ([0, 1], [0, 2, 1], BAD_CU), ([0, 1], [1, 1, 2], BAD_CU), ([0, 1], [-1, 0, 2], BAD_CU),
+                                           ([0, 2], [0, 1, 66], OUT_OF_PAGES), ([0, 1], [0, 2147483647, 2147483647], OUT_OF_PAGES)])
+def test_extend_refuses(slots, cu, code):
+    cache, pool, ws, pages = make(30, 16, 6, 4)
+    extend(cache, pool, ws, [0, 1], [20, 16])
+    status = CU.status_word()
+    past = binding.radix_cache_extend(cache, CU.i32(cu), ws, slots=CU.i32(slots), status=status)
+    assert past.tolist() == [-1] * len(slots) and int(status) == code
+    pool.agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+
+
+@pytest.mark.parametrize("parents,children,code", [([0, 0], [2, 2], BAD_SLOT), ([0], [1], BAD_SLOT), ([0], [0], BAD_SLOT),
+                                                   ([0, 2], [2, 3], BAD_SLOT), ([0], [6], BAD_SLOT), ([-1], [2], BAD_SLOT)])
+def test_fork_refuses(parents, children, code):
+    cache, pool, ws, pages = make(30, 16, 6, 4)
+    extend(cache, pool, ws, [0, 1], [20, 16])
+    status = CU.status_word()
+    binding.radix_cache_fork(cache, CU.i32(parents), CU.i32(children), ws, status=status)
+    assert int(status) == code
+    pool.agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+
+
+def test_free_of_a_slot_twice_and_of_broken_rows():
+    cache, pool, ws, _ = make(30, 16, 6, 4)
+    extend(cache, pool, ws, [0, 1, 2], [50, 30, 5])
+    status = CU.status_word()
+    binding.radix_cache_free(cache, CU.i32([0, 1, 0]), keep_lens=CU.i32([33, -4, 17]), status=status)
+    pool.free([0, 1], [17, 0])
+    pool.agrees(cache)
+    assert int(status) == 0
+    cache.page_table[2, 1] = 30                                              # no page
+    cache.page_table[2, 2] = 29                                              # a page that nobody holds
+    binding.radix_cache_free(cache, CU.i32([2, 6]), status=status)
+    pool.free([2])
+    pool.agrees(cache)
+    assert int(status) in (BAD_PAGE, BAD_SLOT)
+
+
+def test_copies_of_pages_and_their_refusals():
+    cache, _, ws, pages = make(40, 32, 1, 1, layers=3, kv=5)
+    src, dst = [3, 3, 7, 39, 0], [1, 2, 30, 38, 20]                          # one source twice
+    status = CU.status_word()
+    binding.radix_cache_copy_pages(cache, CU.i32(src), CU.i32(dst), ws, status=status)
+    pages[:, dst] = pages[:, src]
+    assert torch.equal(cache.pages.cpu(), pages) and int(status) == 0
+    for src, dst in [([1, 2], [5, 5]), ([1, 2], [2, 6]), ([4], [4]), ([40], [1]), ([1], [-1])]:
+        status.zero_()
+        binding.radix_cache_copy_pages(cache, CU.i32(src), CU.i32(dst), ws, status=status)
+        assert int(status) == BAD_PAGE and torch.equal(cache.pages.cpu(), pages)
+    binding.radix_cache_copy_pages(cache, CU.i32([]), CU.i32([]), ws)
+
+
+def test_compaction_reports_entries_without_a_page():
+    cache, pool, ws, pages = make(12, 16, 3, 4)
+    extend(cache, pool, ws, [0, 1, 2], [30, 30, 30])
+    binding.radix_cache_free(cache, CU.i32([0]))
+    pool.free([0])
+    cache.page_table[0, 3] = 11                                              # a free page behind the used ones
+    status = CU.status_word()
+    used = binding.radix_cache_compact(cache, ws, status=status)
+    assert int(used) == pool.compact(pages) == 4 and int(status) == BAD_PAGE
+    pool.table[0][3] = 11
+    pool.agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+
+
+def test_reset():
+    cache, pool, ws, pages = make(12, 16, 3, 4)
+    extend(cache, pool, ws, [0, 1, 2], [30, 30, 30])
+    binding.radix_cache_reset(cache)
+    CU.Pool(12, 16, 3, 4).agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+
+
+# ---- append
+
+@pytest.mark.parametrize("dtype,hd,kv,page", [("bf16", 128, 8, 16), ("f16", 128, 1, 256), ("f32", 64, 2, 32), ("f32", 4, 3, 16), ("f32", 100, 1, 64)])
+@pytest.mark.parametrize("fused", [False, True])
+def test_append_writes_its_rows_and_nothing_else(dtype, hd, kv, page, fused):
+    past, news = [0, 15, 33, 5, 300], [1, 40, 0, 17, 70]
+    lens = [p + n for p, n in zip(past, news)]
+    cache = CU.random_cache(5, lens, kv, hd, page, dtype, layers=2)
+    want = cache.pages.cpu().clone()
+    cu = CU.ragged(news)
+    N = cu[-1] + 3                                                           # three rows that belong to no sequence
+    past[3] = -1                                                             # a sequence that is left out
+    if fused:
+        row = torch.randn((N, 3 * kv * hd), device="cuda").to(CU.DT[dtype])
+        k, v = row[:, kv * hd:2 * kv * hd].view(N, kv, hd), row[:, 2 * kv * hd:].view(N, kv, hd)
+    else:
+        k, v = (torch.randn((N, kv, hd), device="cuda").to(CU.DT[dtype]) for _ in range(2))
+    status = CU.status_word()
+    binding.radix_cache_append(cache, 1, k, v, CU.i32(cu), CU.i32(past), status=status)
+    table = cache.page_table.tolist()
+    for b in range(len(news)):
+        for i in range(news[b] if past[b] >= 0 else 0):
+            p = past[b] + i
+            want[1, table[b][p // page], 0, :, p % page] = k[cu[b] + i].cpu()
+            want[1, table[b][p // page], 1, :, p % page] = v[cu[b] + i].cpu()
+    assert torch.equal(cache.pages.cpu(), want) and int(status) == 0
+
+
+def test_append_leaves_out_what_has_no_place():
+    cache = CU.random_cache(6, [10, 20, 30], 2, 128, 16, "bf16")
+    want = cache.pages.cpu().clone()
+    k, v = (torch.randn((6, 2, 128), device="cuda").bfloat16() for _ in range(2))
+    for past, slots, cu, code in [([16, 0, 0], [0, 1, 2], [0, 1, 1, 1], BAD_PAGE), ([1 << 30, 0, 0], [0, 1, 2], [0, 1, 1, 1], BAD_PAGE),
+                                  ([0, 0, 0], [3, 1, 2], [0, 1, 1, 1], BAD_SLOT), ([0, 0, 0], [0, 1, -1], [0, 0, 0, 2], BAD_SLOT),
+                                  ([0, 0, 0], [0, 1, 2], [0, 0, 0, 7], BAD_CU)]:
+        status = CU.status_word()
+        binding.radix_cache_append(cache, 0, k, v, CU.i32(cu), CU.i32(past), slots=CU.i32(slots), status=status)
+        assert int(status) == code
+        assert torch.equal(cache.pages.cpu(), want)
+
+
+def test_page_calls_replay_from_a_captured_graph_on_another_stream():
+    cache, pool, ws, pages = make(60, 16, 12, 4)
+    extend(cache, pool, ws, [0, 1], [40, 17])
+    par, kids, cu = CU.i32([0, 1, 0]), CU.i32([5, 6, 7]), CU.i32([0, 1, 9, 10])
+    k, v = (torch.randn((10, 2, 128), device="cuda").bfloat16() for _ in range(2))
+    past, used, status = CU.i32([0, 0, 0]), CU.i32([0]), CU.status_word()
+
+    def calls():
+        binding.radix_cache_free(cache, kids, status=status)
+        binding.radix_cache_fork(cache, par, kids, ws, status=status)
+        binding.radix_cache_extend(cache, cu, ws, slots=kids, past=past, status=status)
+        binding.radix_cache_append(cache, 1, k, v, cu, past, slots=kids, status=status)
+        binding.radix_cache_compact(cache, ws, n_used=used, status=status)
+
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            calls()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        pool.free([5, 6, 7])
+        pool.fork([0, 1, 0], [5, 6, 7], pages)
+        assert past.tolist() == pool.extend([5, 6, 7], [1, 8, 1], pages)
+        for b, (s, n, at) in enumerate([(5, 1, 0), (6, 8, 1), (7, 1, 9)]):
+            for i in range(n):
+                p = pool.lens[s] - n + i
+                pages[1, pool.table[s][p // 16], 0, :, p % 16] = k[at + i].cpu()
+                pages[1, pool.table[s][p // 16], 1, :, p % 16] = v[at + i].cpu()
+        assert int(used) == pool.compact(pages)
+        pool.agrees(cache)
+        assert torch.equal(cache.pages.cpu(), pages) and int(status) == 0
+        torch.randn((100,), device="cuda").sum().item()                      # eager work between the replays
