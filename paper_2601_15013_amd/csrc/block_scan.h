@@ -6,13 +6,25 @@ namespace {
 
 constexpr int PT = 1024;                // threads of such a workgroup
 
-__device__ __forceinline__ int wave_inclusive(int v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(v, o, 64);
-        if (lane >= o) v += u;
-    }
+// x of the lane `ctrl` says (a DPP pattern), 0 where there is none.
+template <int CTRL, int ROWS> __device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ float from_lane(float x) {
+    return __uint_as_float((uint32_t)from_lane<CTRL, ROWS>((int)__float_as_uint(x)));
+}
+// Inclusive sums over the wavefront, in registers: shifts by 1, 2, 4, 8 within rows of 16 lanes, then the last lane of a row to the next
+// one, then of the lower half to the upper.  (Six shuffles through LDS take some ten times as long.)
+template <typename T> __device__ __forceinline__ T wave_inclusive(T v) {
+    v += from_lane<0x111, 0xf>(v);
+    v += from_lane<0x112, 0xf>(v);
+    v += from_lane<0x114, 0xf>(v);
+    v += from_lane<0x118, 0xf>(v);
+    v += from_lane<0x142, 0xa>(v);
+    v += from_lane<0x143, 0xc>(v);
     return v;
+}
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_inclusive(v), 63); }
+__device__ __forceinline__ float wave_total(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(wave_inclusive(v)), 63));
 }
 
 // Exclusive sum of v over the workgroup (all threads call); *total is the sum over all threads.

@@ -171,7 +171,7 @@ extern "C" int radix_paged_attention(const radix_cache* cache, int32_t layer, co
     s.out_stride = (size_t)out_stride;
     const PagedLayout L = paged_layout(c, cache->dtype, s);
     if (ws_bytes < L.total) return RADIX_ERR_WORKSPACE_TOO_SMALL;
-    if (L.few_items > INT32_MAX || L.many_items > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
+    if (L.items > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
     launch_paged_plan(c, s, L, cu_seqlens, past, slots, ws, status_dev, (hipStream_t)stream);
     launch_paged_attention(c, cache->dtype, layer, s, L, q, cu_seqlens, past, slots, out, ws, status_dev, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());

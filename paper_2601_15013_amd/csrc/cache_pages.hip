@@ -41,7 +41,7 @@ __device__ __forceinline__ int number_pages(const int32_t* __restrict__ refs, in
         if (lane < 4) cnt[par][lane * 16 + wave] = mine_of;
         __syncthreads();
         const int mine = cnt[par][lane];                    // lane = 16 u + wavefront: the order of the pages
-        const int incl = wave_inclusive(mine, lane);
+        const int incl = wave_inclusive(mine);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int before = __shfl(incl - mine, u * 16 + wave, 64);

@@ -264,19 +264,18 @@ void launch_cache_append(const CacheView& c, int layer, const void* k, const voi
 
 // Attention of new tokens over the cache.  Sequence b has n = cu[b + 1] - cu[b] new tokens behind past[b] cached ones; its
 // rows - (token, query head of the group) pairs of one kv head, token-major - are cut into blocks.  Sequences of up to
-// `few_rows` rows are walked by the kernel for few rows (and all of them with fp32), the others by the kernel for many.  A block's
-// keys are split over several workgroups where the batch has too few blocks for the chip; their results are joined afterwards.
-// plan[] (int32): {split length of the few kernel in its tiles, of the many kernel}, then prefix sums over the sequences: items of
-// either kernel, units of the join (blocks that are split), partial results of either kernel; the number of splits.
+// `few_rows` rows are walked in the manner for few rows (and all of them with fp32), the others in that for many.  A block's keys are
+// split over several workgroups where the batch has too few blocks for the chip; their results are joined afterwards.
 struct PagedShape {
     int n_q_heads, B, N, max_new;
     size_t q_stride, out_stride;         // elements between tokens
 };
+// Workspace: prefix sums over the sequences (int32 words; batches too large to be planned by every workgroup) and the partial results.
 struct PagedLayout {
-    size_t item_few, item_many, unit, slot_few, slot_many, splits, total_words;  // int32 words
+    size_t item_few, item_many, join, slot, splits;                              // int32 words
     size_t few_acc, few_ml, many_acc, many_ml, total;                            // bytes
-    int few_rows, few_tile, many;        // rows of a block / keys of a tile of the few kernel; whether the many kernel can have work
-    long long few_items, many_items, few_slots, many_slots, units;               // upper bounds
+    int few_rows, few_tile, many;        // rows of a block / keys of a tile for few rows; whether there can be blocks of many rows
+    long long items, few_slots, many_slots, joins;                           // upper bounds
 };
 PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s);
 // plan: the lists above (words of `ws`), and the check of cu, past and slots: a sequence that fails it gets zeros (or nothing, if its

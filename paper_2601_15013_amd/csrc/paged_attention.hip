@@ -23,111 +23,257 @@ constexpr int FEW_TARGET = 1024, MANY_TARGET = 512;      // workgroups that a ba
 constexpr int MANY_ROWS = 128, MANY_TILE = 64;
 constexpr int MAX_HD = 128;
 
+// Up to PLAN_INLINE sequences every workgroup works out the plan by itself, 64 of them at a time; more are planned by a launch of
+// their own.  A plan launch took 8 us, a third of a short sequence's call.
+constexpr int PLAN_INLINE = 256;
+
 struct PagedArgs {
     CacheView c;
     PagedShape s;
     PagedLayout L;
     const int32_t *cu, *past, *slots;
     int layer;
-    const int32_t* plan;
+    int32_t* plan;
     float *few_acc, *few_ml, *many_acc, *many_ml;
 };
 
-// What a sequence of the batch has, from device data that may be anything: `from` .. `from + n` lies in [0, N), and len <= what the
-// table's row can hold.  len = 0: nothing to attend to (zeros).
-struct PagedSeq { int from, n, len, past, row, err; };
+// What a sequence of the batch has, from device data that may be anything: `from` .. `from + n` lies in [0, N), and len = past + n <=
+// what the table's row can hold.  len = 0: nothing to attend to (zeros).
+struct PagedSeq { int from, n, len, row, err; };
 __device__ __forceinline__ PagedSeq paged_seq(const CacheView& c, const PagedShape& s, const int32_t* cu, const int32_t* past,
                                               const int32_t* slots, int b) {
-    PagedSeq q;
     const int from = cu[b], to = cu[b + 1];
     const int p = past[b], row = slots ? slots[b] : b;
-    q.err = 0;
-    q.from = from; q.n = 0; q.len = 0; q.past = 0; q.row = 0;
-    if (from < 0 || to < from || to > s.N || (long long)to - from > s.max_new) { q.from = 0; q.err = RADIX_ERR_BAD_CU_SEQLENS; return q; }
+    PagedSeq q = {0, 0, 0, 0, 0};
+    if (from < 0 || to < from || to > s.N || (long long)to - from > s.max_new) { q.err = RADIX_ERR_BAD_CU_SEQLENS; return q; }
+    q.from = from;
     q.n = to - from;
     if (p < 0 || q.n == 0) return q;
     if (row < 0 || row >= c.max_seqs) { q.err = RADIX_ERR_BAD_SLOT; return q; }
     if ((long long)p + q.n > (long long)c.max_pages * c.page_size) { q.err = RADIX_ERR_BAD_PAGE; return q; }
     q.row = row;
-    q.past = p;
     q.len = p + q.n;
     return q;
 }
 
-// ------------------------------------------------------------------ the plan (one workgroup)
+// How a sequence is cut: by which kernel, into how many blocks of rows, and tiles of keys up to its last position.
+struct PagedCut { bool few; int blocks, tiles; };
+__device__ __forceinline__ PagedCut paged_cut(const CacheView& c, const PagedShape& s, const PagedLayout& L, const PagedSeq& q) {
+    const int rows = q.n * (s.n_q_heads / c.n_kv_heads);
+    PagedCut k;
+    k.few = !L.many || rows <= L.few_rows;
+    k.blocks = k.few ? (rows + L.few_rows - 1) >> (L.few_rows == 16 ? 4 : 5) : (rows + MANY_ROWS - 1) / MANY_ROWS;
+    k.tiles = (q.len >> 4) + ((q.len & 15) != 0);                // of 16 keys
+    k.tiles = k.few ? (L.few_tile == 16 ? k.tiles : (k.tiles + 1) >> 1) : (k.tiles + 3) >> 2;
+    return k;
+}
+// Tiles of a split: an even share of the work for the target number of workgroups, and no less than pays for writing and joining the
+// parts: 256 keys with few rows, 1024 with many, whose parts of 64 KB cost what six tiles do.  With few rows, which are bound by memory
+// and want to be even, a sequence is cut into ceil(tiles / length) parts, with many into floor(tiles / length).
+// (The sum of the work is a float: its rounding is covered by the factor, so that the parts of split blocks are fewer than twice the
+// target, or than the target, for which there is room.)
+__device__ __forceinline__ int split_length(float work, int target, int least) {
+    const int share = (int)ceilf(work * (1.0001f / (float)target));
+    return share > least ? share : least;
+}
+__device__ __forceinline__ int few_length(float work, int tile) { return split_length(work, FEW_TARGET, 256 / tile); }
+__device__ __forceinline__ int many_length(float work) { return split_length(work, MANY_TARGET, 1024 / MANY_TILE); }
+__device__ __forceinline__ int splits_of(const PagedCut& k, int few_len, int many_len) {
+    const int length = k.few ? few_len : many_len, n = (int)((unsigned)(k.tiles + (k.few ? length - 1 : 0)) / (unsigned)length);
+    return n > 1 ? n : 1;
+}
+// Entries of the join for a split sequence: some rows of a kv head each, which all lie in one block.  With few parts eight rows are joined
+// side by side, with more of them one after the other.
+constexpr int JOIN_ALONE = 8;
+__device__ __forceinline__ int join_step(int splits) { return splits > JOIN_ALONE ? 1 : 8; }
+__device__ __forceinline__ int join_rows(bool few, int splits) { return join_step(splits) * (few ? 1 : splits > JOIN_ALONE ? 8 : 4); }
+__device__ __forceinline__ int join_entries(bool few, int rows, int kv, int splits) {
+    const int step = join_rows(few, splits);
+    return splits <= 1 ? 0 : (rows + step - 1) / step * kv;
+}
+
+// ------------------------------------------------------------------ the plan as a launch of its own (one workgroup)
 __global__ __launch_bounds__(PT) void paged_plan_kernel(CacheView c, PagedShape s, PagedLayout L, const int32_t* __restrict__ cu,
                                                         const int32_t* __restrict__ past, const int32_t* __restrict__ slots,
                                                         int32_t* __restrict__ plan, int32_t* status) {
     __shared__ long long part[PT / 64];
-    const int tid = threadIdx.x, group = s.n_q_heads / c.n_kv_heads;
-    auto shape_of = [&](int b, bool& few, int& blocks, int& tiles) -> int {
-        const PagedSeq q = paged_seq(c, s, cu, past, slots, b);
-        const int rows = q.n * group;
-        few = !L.many || rows <= L.few_rows;
-        blocks = few ? ceil_div(rows, L.few_rows) : ceil_div(rows, MANY_ROWS);
-        tiles = few ? ceil_div(q.len, L.few_tile) : ceil_div(q.len, MANY_TILE);
-        return q.err;
-    };
-    long long few_work = 0, many_work = 0, total;
+    __shared__ float work[2][PT / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, group = s.n_q_heads / c.n_kv_heads;
+    float few_work = 0.f, many_work = 0.f;
     for (int b = tid; b < s.B; b += PT) {
-        bool few; int blocks, tiles;
-        const int err = shape_of(b, few, blocks, tiles);
-        if (err) set_status(status, err);
-        (few ? few_work : many_work) += (long long)blocks * tiles * c.n_kv_heads;
+        const PagedSeq q = paged_seq(c, s, cu, past, slots, b);
+        const PagedCut k = paged_cut(c, s, L, q);
+        if (q.err) set_status(status, q.err);
+        const float w = (float)k.blocks * (float)k.tiles * (float)c.n_kv_heads;
+        few_work += k.few ? w : 0.f;
+        many_work += k.few ? 0.f : w;
     }
-    block_exclusive(few_work, &total, part);
-    // tiles of a split: even shares of the work for the target number of workgroups, no less than 256 keys
-    const long long least_few = 256 / L.few_tile, least_many = 256 / MANY_TILE;
-    const long long few_len = max(least_few, (total + FEW_TARGET - 1) / FEW_TARGET);
-    block_exclusive(many_work, &total, part);
-    const long long many_len = max(least_many, (total + MANY_TARGET - 1) / MANY_TARGET);
-    long long run_items = 0, run_slots = 0, run_units = 0;               // few in the low half, many in the high half
+    few_work = wave_sum(few_work);
+    many_work = wave_sum(many_work);
+    if (lane == 0) { work[0][wave] = few_work; work[1][wave] = many_work; }
+    __syncthreads();
+    few_work = many_work = 0.f;
+    for (int w = 0; w < PT / 64; ++w) { few_work += work[0][w]; many_work += work[1][w]; }
+    const int few_len = few_length(few_work, L.few_tile), many_len = many_length(many_work);
+    long long run_items = 0, run_slots = 0, run_rows = 0;               // few in the low half, many in the high half
     for (int b0 = 0; b0 < s.B; b0 += PT) {
         const int b = b0 + tid;
-        bool few = true; int blocks = 0, tiles = 0, splits = 1;
+        PagedCut k = {true, 0, 0};
+        int splits = 1, rows = 0;
         if (b < s.B) {
-            shape_of(b, few, blocks, tiles);
-            splits = (int)((tiles + (few ? few_len : many_len) - 1) / (few ? few_len : many_len));
-            splits = splits < 1 ? 1 : splits;
+            const PagedSeq q = paged_seq(c, s, cu, past, slots, b);
+            k = paged_cut(c, s, L, q);
+            splits = splits_of(k, few_len, many_len);
+            rows = q.n * group;
         }
-        const long long units = (long long)blocks * c.n_kv_heads, items = units * splits;
-        const int sh = few ? 0 : 32;
-        long long ti, ts, tu;
+        const long long items = (long long)k.blocks * c.n_kv_heads * splits;
+        const int sh = k.few ? 0 : 32;
+        long long ti, ts, tr;
         const long long i0 = run_items + block_exclusive(items << sh, &ti, part);
         const long long s0 = run_slots + block_exclusive((splits > 1 ? items : 0) << sh, &ts, part);
-        const long long u0 = run_units + block_exclusive(splits > 1 ? units : 0, &tu, part);
+        const long long r0 = run_rows + block_exclusive(join_entries(k.few, rows, c.n_kv_heads, splits), &tr, part);
         if (b < s.B) {
             plan[L.item_few + b] = (int)(i0 & 0xffffffffLL);
             plan[L.item_many + b] = (int)(i0 >> 32);
-            plan[L.slot_few + b] = (int)(s0 & 0xffffffffLL);
-            plan[L.slot_many + b] = (int)(s0 >> 32);
-            plan[L.unit + b] = (int)u0;
+            plan[L.slot + b] = (int)(k.few ? s0 & 0xffffffffLL : s0 >> 32);
+            plan[L.join + b] = (int)r0;
             plan[L.splits + b] = splits;
         }
-        run_items += ti; run_slots += ts; run_units += tu;
+        run_items += ti; run_slots += ts; run_rows += tr;
     }
     if (tid == 0) {
         plan[L.item_few + s.B] = (int)(run_items & 0xffffffffLL);
         plan[L.item_many + s.B] = (int)(run_items >> 32);
-        plan[L.unit + s.B] = (int)run_units;
+        plan[L.join + s.B] = (int)run_rows;
     }
 }
 
-// A work item: the kv head, block and tile range of a sequence; `slot` of its partial result where the block is split.
+// One entry of the batch's list of items (those of many rows first): its sequence, the entry's number within the sequence, the
+// sequence's splits and where its partial results begin.  By a wavefront.
+struct PagedFound { PagedSeq q; bool few; int in, blocks, splits, slot; };
+// From the lists in the workspace.
+__device__ __forceinline__ bool paged_listed(const PagedArgs& a, int index, int lane, PagedFound& f) {
+    const int32_t* many = a.plan + a.L.item_many;
+    const int n_many = many[a.s.B];
+    const int32_t* first = index < n_many ? many : a.plan + a.L.item_few;
+    if (index >= n_many) index -= n_many;
+    if (index >= first[a.s.B]) return false;
+    const int b = __builtin_amdgcn_readfirstlane(sequence_of(first, a.s.B, index, lane));
+    f.in = index - first[b];
+    f.splits = a.plan[a.L.splits + b];
+    f.slot = a.plan[a.L.slot + b];
+    f.q = paged_seq(a.c, a.s, a.cu, a.past, a.slots, b);
+    const PagedCut k = paged_cut(a.c, a.s, a.L, f.q);
+    f.few = k.few;
+    f.blocks = k.blocks;
+    return true;
+}
+// Worked out on the spot, 64 sequences at a time; the first 64, which are often all, stay in registers between the passes.  Workgroup 0
+// reports what cannot be and leaves the join its lists.
+__device__ __forceinline__ bool paged_planned(const PagedArgs& a, int index, int lane, PagedFound& f, int32_t* plan, int32_t* status) {
+    const int kv = a.c.n_kv_heads, group = a.s.n_q_heads / kv;
+    const bool writer = blockIdx.x == 0 && threadIdx.x < 64;
+    PagedSeq q;
+    PagedCut k;
+    auto fetch = [&](int b) {
+        q = {0, 0, 0, 0, 0};
+        k = {true, 0, 0};
+        if (b < a.s.B) {
+            q = paged_seq(a.c, a.s, a.cu, a.past, a.slots, b);
+            k = paged_cut(a.c, a.s, a.L, q);
+        }
+    };
+    const int last = (a.s.B - 1) & ~63;
+    float few_work = 0.f, many_work = 0.f;
+#pragma unroll 1
+    for (int b0 = last; b0 >= 0; b0 -= 64) {
+        fetch(b0 + lane);
+        if (writer && q.err) set_status(status, q.err);
+        const float w = (float)k.blocks * (float)k.tiles * (float)kv;
+        few_work += k.few ? w : 0.f;
+        many_work += k.few ? 0.f : w;
+    }
+    const int few_len = few_length(wave_total(few_work), a.L.few_tile);
+    int many_len = 1;
+    bool few = true;
+    if (a.L.many) {
+        many_len = many_length(wave_total(many_work));
+        int n_many = 0;
+#pragma unroll 1
+        for (int b0 = last; b0 >= 0; b0 -= 64) {
+            if (last > 0) fetch(b0 + lane);
+            n_many += k.few ? 0 : k.blocks * kv * splits_of(k, 1, many_len);
+        }
+        n_many = wave_total(n_many);
+        few = index >= n_many;
+        if (few) index -= n_many;
+    }
+    int at = 0, at_few = 0, at_many = 0, at_join = 0;
+    bool found = false;
+#pragma unroll 1
+    for (int b0 = 0; b0 <= last; b0 += 64) {
+        if (b0 > 0) fetch(b0 + lane);
+        const int splits = splits_of(k, few_len, many_len);
+        const int items = k.blocks * kv * splits, parts = splits > 1 ? items : 0;
+        const int mine = k.few == few ? items : 0;
+        const int incl = wave_inclusive(mine) + at;
+        const int few_parts = wave_inclusive(k.few ? parts : 0) + at_few;
+        int many_parts = at_many;
+        if (a.L.many) many_parts += wave_inclusive(k.few ? 0 : parts);
+        const int slot = (k.few ? few_parts : many_parts) - parts;
+        if (writer) {
+            const int joins = join_entries(k.few, q.n * group, kv, splits), join_incl = wave_inclusive(joins) + at_join;
+            if (b0 + lane < a.s.B) {
+                plan[a.L.join + b0 + lane + 1] = join_incl;
+                plan[a.L.slot + b0 + lane] = slot;
+                plan[a.L.splits + b0 + lane] = splits;
+                if (b0 + lane == 0) plan[a.L.join] = 0;
+            }
+            at_join = __builtin_amdgcn_readlane(join_incl, 63);
+        }
+        const unsigned long long hit = __ballot(index < incl && index >= incl - mine);
+        if (hit && !found) {
+            const int l = __ffsll((long long)hit) - 1;
+            found = true;
+            f.few = __builtin_amdgcn_readlane((int)k.few, l) != 0;
+            f.in = index - __builtin_amdgcn_readlane(incl - mine, l);
+            f.blocks = __builtin_amdgcn_readlane(k.blocks, l);
+            f.splits = __builtin_amdgcn_readlane(splits, l);
+            f.slot = __builtin_amdgcn_readlane(slot, l);
+            f.q.from = __builtin_amdgcn_readlane(q.from, l);
+            f.q.n = __builtin_amdgcn_readlane(q.n, l);
+            f.q.len = __builtin_amdgcn_readlane(q.len, l);
+            f.q.row = __builtin_amdgcn_readlane(q.row, l);
+            if (!writer) break;
+        }
+        at = __builtin_amdgcn_readlane(incl, 63);
+        at_few = __builtin_amdgcn_readlane(few_parts, 63);
+        at_many = __builtin_amdgcn_readlane(many_parts, 63);
+    }
+    return found;
+}
+// (sums over a malformed cu_seqlens may have wrapped: nothing leaves the lists' room)
+__device__ __forceinline__ bool paged_find(const PagedArgs& a, int lane, PagedFound& f, int32_t* status) {
+    const bool found = a.s.B > PLAN_INLINE ? paged_listed(a, blockIdx.x, lane, f) : paged_planned(a, blockIdx.x, lane, f, a.plan, status);
+    if (!found) return false;
+    const long long items = (long long)f.blocks * a.c.n_kv_heads * f.splits;
+    return f.in >= 0 && f.in < items && (f.splits == 1 || (f.slot >= 0 && f.slot + items <= (f.few ? a.L.few_slots : a.L.many_slots)));
+}
+
+// A work item: the kv head, block and split of a sequence; `slot` of its partial result where the block is split.
 // Items of a sequence: kv heads fastest, so that consecutive workgroups - and with them the eight XCDs - take different heads, and
 // the blocks of one head, which read the same keys, meet in one L2; then the splits; then the blocks, the last (longest) first.
-struct PagedItem { int b, kvh, blk, split, splits, slot; };
-__device__ __forceinline__ bool paged_item(const PagedArgs& a, size_t item_at, size_t slot_at, long long max_slots, int item, int lane, PagedItem& w) {
-    const int32_t* first = a.plan + item_at;
-    if (item >= first[a.s.B]) return false;
-    w.b = __builtin_amdgcn_readfirstlane(sequence_of(first, a.s.B, item, lane));
-    const int begin = first[w.b], in = item - begin, items = first[w.b + 1] - begin;
-    w.splits = a.plan[a.L.splits + w.b];
-    w.kvh = in % a.c.n_kv_heads;
-    w.split = in / a.c.n_kv_heads % w.splits;
-    w.blk = items / a.c.n_kv_heads / w.splits - 1 - in / a.c.n_kv_heads / w.splits;
-    w.slot = a.plan[slot_at + w.b] + in;
-    return in >= 0 && w.blk >= 0 && (w.splits == 1 || (w.slot >= 0 && w.slot < max_slots));    // (sums over a malformed cu may wrap)
+struct PagedItem { PagedSeq q; int kvh, blk, split, splits, slot; };
+__device__ __forceinline__ PagedItem paged_item(const PagedArgs& a, const PagedFound& f) {
+    const int kv = a.c.n_kv_heads, rest = f.in / kv;
+    PagedItem w;
+    w.q = f.q;
+    w.kvh = f.in - rest * kv;
+    w.splits = f.splits;
+    w.split = rest % f.splits;
+    w.blk = f.blocks - 1 - rest / f.splits;
+    w.slot = f.slot + f.in;
+    return w;
 }
 
 // A table entry is fetched well before it is needed and checked where it is: one that is no page becomes page 0 and is reported.
@@ -294,24 +440,26 @@ template <int HC> struct FewTileF32 {                                         //
     static __device__ __forceinline__ int element_of(int a, int i, int lane) { return 64 * (a >> 2) + 4 * (4 * (lane >> 4) + i) + (a & 3); }
 };
 
+template <typename Tile, int NT> struct FewShared {
+    float o[4][16 * NT][MAX_HD + 4];
+    float m[4][16 * NT], l[4][16 * NT];
+};
 template <typename Tile, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_few_kernel(PagedArgs a, const typename Tile::T* __restrict__ q,
-                                                           typename Tile::T* __restrict__ out, int32_t* status) {
+__device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w, const typename Tile::T* __restrict__ q,
+                                         typename Tile::T* __restrict__ out, FewShared<Tile, NT>& sh, int32_t* status) {
     typedef typename Tile::T T;
-    constexpr int NA = Tile::NA;
-    constexpr int ROWS = 16 * NT, PITCH = MAX_HD + 4;
-    __shared__ float so[4][ROWS][PITCH];
-    __shared__ float sm[4][ROWS], sl[4][ROWS];
+    constexpr int NA = Tile::NA, ROWS = 16 * NT;
+    auto &so = sh.o;
+    auto &sm = sh.m, &sl = sh.l;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15;
-    PagedItem w;
-    if (!paged_item(a, a.L.item_few, a.L.slot_few, a.L.few_slots, blockIdx.x, lane, w)) return;
-    const PagedSeq sq = paged_seq(a.c, a.s, a.cu, a.past, a.slots, w.b);
+    const PagedSeq& sq = w.q;
+    const int past = sq.len - sq.n;                         // (len = 0: unused)
     const int hd = a.c.head_dim, group = a.s.n_q_heads / a.c.n_kv_heads, rows = sq.n * group;
     const int row0 = w.blk * ROWS, last = sq.len - 1;
     // the item's tiles: its share of those up to the last position that a row of the block sees
     const int last_row = min(row0 + ROWS, rows) - 1;
-    const int tiles = sq.len > 0 ? (sq.past + last_row / group) / Tile::KEYS + 1 : 0;
+    const int tiles = sq.len > 0 ? (past + last_row / group) / Tile::KEYS + 1 : 0;
     const int t0 = (int)((long long)tiles * w.split / w.splits), t1 = (int)((long long)tiles * (w.split + 1) / w.splits);
     const int32_t* table = a.c.table + (size_t)sq.row * a.c.max_pages;
     const char* base = a.c.pages + (size_t)a.layer * a.c.layer_bytes + (size_t)w.kvh * a.c.piece_bytes;
@@ -321,7 +469,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_few_kernel(PagedAr
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int row = row0 + 16 * nt + r, j = min(row, last_row) / group, h = w.kvh * group + min(row, last_row) % group;
-        limit[nt] = sq.past + j;
+        limit[nt] = past + j;
         tile.load_q(q + (size_t)(sq.from + j) * a.s.q_stride + (size_t)h * hd, nt, row <= last_row, hd, lane);
     }
     f32x4 acc[NT][NA];
@@ -439,23 +587,25 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_few_kernel(PagedAr
 // kernel: S^T = K Q^T with 32x32x16 matrix instructions, so that a lane owns one row; O^T = V^T P^T with V^T read by transposing reads.
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
+struct ManyShared {
+    uint4 K[2][MANY_TILE * 16];                              // chunk (8 elements) ^= key & 15
+    uint4 V[2][MANY_TILE * 16];                              // chunk ^= (key & 3) << 2
+};
 template <int DT>
-__global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, const typename Op<DT>::T* __restrict__ q,
-                                                            typename Op<DT>::T* __restrict__ out, int32_t* status) {
+__device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedItem& w, const typename Op<DT>::T* __restrict__ q,
+                                          typename Op<DT>::T* __restrict__ out, ManyShared& sh, int32_t* status) {
     typedef typename Op<DT>::T T;
     typedef typename Op<DT>::V8 V8;
     typedef typename Op<DT>::V4 V4;
     constexpr int HD = MAX_HD, BKV = MANY_TILE;
-    __shared__ uint4 Ks[2][BKV * 16];                        // chunk (8 elements) ^= key & 15
-    __shared__ uint4 Vs[2][BKV * 16];                        // chunk ^= (key & 3) << 2
+    auto &Ks = sh.K, &Vs = sh.V;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
-    PagedItem w;
-    if (!paged_item(a, a.L.item_many, a.L.slot_many, a.L.many_slots, blockIdx.x, lane, w)) return;
-    const PagedSeq sq = paged_seq(a.c, a.s, a.cu, a.past, a.slots, w.b);
+    const PagedSeq& sq = w.q;
+    const int past = sq.len - sq.n;                          // (len = 0: unused)
     const int group = a.s.n_q_heads / a.c.n_kv_heads, rows = sq.n * group;
     const int row0 = w.blk * MANY_ROWS, last_row = min(row0 + MANY_ROWS, rows) - 1;
-    const int tiles = sq.len > 0 ? (sq.past + last_row / group) / BKV + 1 : 0;
+    const int tiles = sq.len > 0 ? (past + last_row / group) / BKV + 1 : 0;
     const int t0 = (int)((long long)tiles * w.split / w.splits), t1 = (int)((long long)tiles * (w.split + 1) / w.splits);
     const int32_t* table = a.c.table + (size_t)sq.row * a.c.max_pages;
     const char* base = a.c.pages + (size_t)a.layer * a.c.layer_bytes + (size_t)w.kvh * a.c.piece_bytes;
@@ -463,10 +613,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, const t
 
     // the wavefront's rows and the positions that its first and last one see
     const int wrow = row0 + 32 * wave;
-    const int qmin = sq.past + min(wrow, last_row) / group;
-    const int qmax = wrow <= last_row ? sq.past + min(wrow + 31, last_row) / group : -1;
+    const int qmin = past + min(wrow, last_row) / group;
+    const int qmax = wrow <= last_row ? past + min(wrow + 31, last_row) / group : -1;
     const int my_row = min(wrow + n, last_row), my_tok = my_row / group, my_head = w.kvh * group + my_row % group;
-    const int limit = sq.past + my_tok;
+    const int limit = past + my_tok;
 
     const int lrow = lane >> 4, lpc = lane & 15;
     auto page_of = [&](int t) { return table[min(t * BKV + 16 * wave, last) >> a.c.page_shift]; };
@@ -618,45 +768,109 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedArgs a, const t
         }
 }
 
-// ------------------------------------------------------------------ join
-// A wavefront joins the parts of one row of a split block, in the order of the keys; a lane owns two elements.
+// ------------------------------------------------------------------ the kernels
+template <typename Tile, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_few_kernel(PagedArgs a, const typename Tile::T* __restrict__ q,
+                                                                         typename Tile::T* __restrict__ out, int32_t* status) {
+    __shared__ FewShared<Tile, NT> sh;
+    PagedFound f;
+    if (!paged_find(a, threadIdx.x & 63, f, status)) return;
+    few_rows<Tile, NT>(a, paged_item(a, f), q, out, sh, status);
+}
+
+// Both kinds of items in one launch: the blocks of many rows first, whose work is the longer.
+template <int DT>
+__global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedArgs a, const typename Op<DT>::T* __restrict__ q,
+                                                             typename Op<DT>::T* __restrict__ out, int32_t* status) {
+    __shared__ union { ManyShared many; FewShared<FewTile<DT, 1>, 1> few; } sh;
+    PagedFound f;
+    if (!paged_find(a, threadIdx.x & 63, f, status)) return;
+    const PagedItem w = paged_item(a, f);
+    if (f.few) few_rows<FewTile<DT, 1>, 1>(a, w, q, out, sh.few, status);
+    else many_rows<DT>(a, w, q, out, sh.many, status);
+}
+
+// Joins the parts of split blocks; workgroups take entries in turn.  Groups of 32 lanes, four elements a lane: with few parts a group joins a row by itself, with more
+// the eight groups take every eighth part of one row and their sums are added in order.
+struct JoinArgs {
+    const int32_t *cu, *first, *splits, *slot;
+    const float *few_acc, *few_ml, *many_acc, *many_ml;
+    int B, N, max_new, kv, group, hd, few_rows, few_slots, many_slots, out_stride;
+    bool many;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, T* __restrict__ out) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int hd = a.c.head_dim, group = a.s.n_q_heads / a.c.n_kv_heads;
-    const int32_t* first = a.plan + a.L.unit;
-    const int units = first[a.s.B];
-    for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int b = __builtin_amdgcn_readfirstlane(sequence_of(first, a.s.B, unit, lane));
-        const PagedSeq sq = paged_seq(a.c, a.s, a.cu, a.past, a.slots, b);
-        const int rows = sq.n * group, splits = a.plan[a.L.splits + b];
-        const bool few = !a.L.many || rows <= a.L.few_rows;
-        const int block = few ? a.L.few_rows : MANY_ROWS;
-        const int in = unit - first[b], kvh = in % a.c.n_kv_heads, back = in / a.c.n_kv_heads;
-        const int blocks = ceil_div(rows, block), blk = blocks - 1 - back;
-        const int row = blk * block + (int)blockIdx.y * 4 + wave;
-        if ((int)blockIdx.y * 4 + wave >= block || row >= rows) continue;
+__global__ __launch_bounds__(256) void paged_join_kernel(JoinArgs a, T* __restrict__ out) {
+    __shared__ f32x4 so[8][MAX_HD / 4];
+    __shared__ float sl[8], sm[4];
+    const int lane = threadIdx.x & 63, part = threadIdx.x >> 5, e = threadIdx.x & 31;
+    const int entries = a.first[a.B];
+#pragma unroll 1
+    for (int index = blockIdx.x; index < entries; index += gridDim.x) {
+        int kv = a.kv, group = a.group;
+        asm volatile("" : "+s"(kv), "+s"(group));          // what their divisions need is made anew: held over the loop it would not fit
+        const int b = __builtin_amdgcn_readfirstlane(sequence_of(a.first, a.B, index, lane));
+        const int in = index - a.first[b], splits = a.splits[b], slot = a.slot[b], from = a.cu[b], n = a.cu[b + 1] - from, rows = n * group;
+        if (from < 0 || n <= 0 || n > a.max_new || from > a.N - n) continue;
+        const bool few = !a.many || rows <= a.few_rows, together = splits > JOIN_ALONE;
+        const int block = few ? a.few_rows : MANY_ROWS, blocks = (rows + block - 1) / block;
+        const int step = join_step(splits), count = join_rows(few, splits);
+        const int kvh = in % kv, row0 = in / kv * count, end = min(row0 + count, rows);
+        if (in < 0 || row0 >= rows || slot < 0 || slot + (long long)blocks * kv * splits > (few ? a.few_slots : a.many_slots)) continue;
         const float* acc = few ? a.few_acc : a.many_acc;
         const float* ml = few ? a.few_ml : a.many_ml;
-        const size_t slot0 = (size_t)a.plan[(few ? a.L.slot_few : a.L.slot_many) + b] + (size_t)back * splits * a.c.n_kv_heads + kvh;
-        auto at = [&](int k) { return (slot0 + (size_t)k * a.c.n_kv_heads) * block + (row - blk * block); };
-        float top = -INFINITY;
-        for (int k = lane; k < splits; k += 64) top = fmaxf(top, ml[2 * at(k)]);
-        top = wave_max(top);
-        const float use = finite_or_zero(top);
-        float sum = 0.f, o0 = 0.f, o1 = 0.f;
-        const int e = 2 * lane < hd ? 2 * lane : hd - 2;
+        int slot0 = slot + (blocks - 1 - row0 / block) * splits * kv + kvh;               // 32 bits hold any place in the parts' room
+        asm volatile("" : "+v"(slot0));                    // (addresses in vector registers: there are plenty)
+#pragma unroll 1
+        for (int r0 = row0; r0 < end; r0 += step) {
+            const int row = together ? r0 : r0 + part;
+            const bool active = row < end;
+            auto at = [&](int k) { return (slot0 + k * kv) * block + (row & (block - 1)); };
+            float top = -INFINITY, sum = 0.f;
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            auto add = [&](int k, float use) {
+                const int i = at(k);
+                const float w = __builtin_amdgcn_exp2f(ml[2 * i] - use);
+                const f32x4 x = *reinterpret_cast<const f32x4*>(acc + i * MAX_HD + 4 * e);  // (elements from head_dim on: unused)
+                sum = fmaf(w, ml[2 * i + 1], sum);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) o[u] = fmaf(w, x[u], o[u]);
+            };
+            if (together) {
+                for (int k = threadIdx.x; k < splits; k += 256) top = fmaxf(top, ml[2 * at(k)]);
+                top = wave_max(top);
+                __syncthreads();                            // the row before is through with LDS
+                if (lane == 0) sm[threadIdx.x >> 6] = top;
+                __syncthreads();
+                const float use = finite_or_zero(fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])));
 #pragma unroll 8
-        for (int k = 0; k < splits; ++k) {
-            const size_t i = at(k);
-            const float f = __builtin_amdgcn_exp2f(ml[2 * i] - use);
-            sum = fmaf(f, ml[2 * i + 1], sum);
-            o0 = fmaf(f, acc[i * MAX_HD + e], o0);
-            o1 = fmaf(f, acc[i * MAX_HD + e + 1], o1);
+                for (int k = part; k < splits; k += 8) add(k, use);
+                so[part][e] = o;
+                if (e == 0) sl[part] = sum;
+                __syncthreads();
+                sum = 0.f;
+                o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    sum += sl[p];
+                    o += so[p][e];
+                }
+            } else if (active) {
+#pragma unroll 4
+                for (int k = 0; k < splits; ++k) top = fmaxf(top, ml[2 * at(k)]);
+                const float use = finite_or_zero(top);
+#pragma unroll 4
+                for (int k = 0; k < splits; ++k) add(k, use);
+            }
+            if (active && (!together || part == 0) && 4 * e < a.hd) {
+                const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
+                T* op = out + (size_t)(from + row / group) * a.out_stride + (size_t)(kvh * group + row % group) * a.hd + 4 * e;
+                T y[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) y[u] = from_f32<T>(o[u] * inv);
+                if (sizeof(T) == 4) *reinterpret_cast<uint4*>(op) = *reinterpret_cast<uint4*>(y);
+                else *reinterpret_cast<uint2*>(op) = *reinterpret_cast<uint2*>(y);
+            }
         }
-        const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
-        T* op = out + (size_t)(sq.from + row / group) * a.s.out_stride + (size_t)(kvh * group + row % group) * hd;
-        if (2 * lane < hd) { op[e] = from_f32<T>(o0 * inv); op[e + 1] = from_f32<T>(o1 * inv); }
     }
 }
 
@@ -666,29 +880,29 @@ PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s) {
     PagedLayout L;
     const int group = s.n_q_heads / c.n_kv_heads;
     const long long most_rows = (long long)s.max_new * group;
-    L.few_rows = dtype == RADIX_F32 || most_rows <= 16 ? 16 : 32;
+    // 16 rows a block, or 32 where the whole batch fits that: then no sequence needs the other kernel.  (Sequences of one token in a batch
+    // with chunks: 84 us in blocks of 32 rows, 61 in blocks of 16, whose wavefronts leave room for a second one per SIMD.)
+    L.few_rows = dtype != RADIX_F32 && most_rows > 16 && most_rows <= 32 ? 32 : 16;
     L.few_tile = dtype == RADIX_F32 ? 16 : 32;
     L.many = dtype != RADIX_F32 && most_rows > L.few_rows;
     const long long N = s.N, B = s.B, kv = c.n_kv_heads;
     // blocks of sequence b: at most rows / block + 1, and none without tokens
-    const long long few_blocks = dtype == RADIX_F32 ? N * group / 16 + B : B, many_blocks = L.many ? N * group / MANY_ROWS + B : 0;
-    L.few_items = few_blocks * kv + FEW_TARGET;
-    L.many_items = L.many ? many_blocks * kv + MANY_TARGET : 0;
-    // a block is split into ceil(tiles / length) > 1 parts, fewer than 2 tiles / length, and the lengths add up to the target
+    const long long few_blocks = dtype == RADIX_F32 ? N * group / 16 + B : (B < N ? B : N), many_blocks = L.many ? N * group / MANY_ROWS + B : 0;
+    L.items = few_blocks * kv + FEW_TARGET + (L.many ? many_blocks * kv + MANY_TARGET : 0);
+    // (ceil(x) < 2 x where it is more than one)
     L.few_slots = 2 * FEW_TARGET;
-    L.many_slots = L.many ? 2 * MANY_TARGET : 0;
-    L.units = FEW_TARGET + (L.many ? MANY_TARGET : 0);
-    if (L.units > (few_blocks + many_blocks) * kv) L.units = (few_blocks + many_blocks) * kv;
+    L.many_slots = L.many ? MANY_TARGET : 0;
+    L.joins = N * s.n_q_heads;                               // entries of the join: a row at the least
     size_t w = 64;
-    L.item_few = w; w += (size_t)B + 1;
-    L.item_many = w; w += (size_t)B + 1;
-    L.unit = w; w += (size_t)B + 1;
-    L.slot_few = w; w += (size_t)B;
-    L.slot_many = w; w += (size_t)B;
-    L.splits = w; w += (size_t)B;
-    L.total_words = w;
+    auto words = [&](size_t n) { const size_t o = w; w += n; return o; };
+    L.item_few = words((size_t)B + 1);
+    L.item_many = words((size_t)B + 1);
+    L.join = words((size_t)B + 1);
+    L.slot = words((size_t)B);
+    L.splits = words((size_t)B);
     size_t off = align_up(w * 4, 256);
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
+    // up to 16 rows a block, or 32: room for either, so that the size grows with max_new
     L.few_acc = take((size_t)L.few_slots * L.few_rows * MAX_HD * 4);
     L.few_ml = take((size_t)L.few_slots * L.few_rows * 8);
     L.many_acc = take((size_t)L.many_slots * MANY_ROWS * MAX_HD * 4);
@@ -699,36 +913,39 @@ PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s) {
 
 void launch_paged_plan(const CacheView& c, const PagedShape& s, const PagedLayout& L, const int32_t* cu, const int32_t* past,
                        const int32_t* slots, void* ws, int32_t* status, hipStream_t stream) {
-    hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(PT), 0, stream, c, s, L, cu, past, slots, (int32_t*)ws, status);
+    if (s.B > PLAN_INLINE)
+        hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(PT), 0, stream, c, s, L, cu, past, slots, (int32_t*)ws, status);
 }
 
 int launch_paged_attention(const CacheView& c, int dtype, int layer, const PagedShape& s, const PagedLayout& L, const void* q,
                            const int32_t* cu, const int32_t* past, const int32_t* slots, void* out, void* ws, int32_t* status,
                            hipStream_t stream) {
     char* w = (char*)ws;
-    PagedArgs a = {c, s, L, cu, past, slots, layer, (const int32_t*)ws, (float*)(w + L.few_acc), (float*)(w + L.few_ml),
+    PagedArgs a = {c, s, L, cu, past, slots, layer, (int32_t*)ws, (float*)(w + L.few_acc), (float*)(w + L.few_ml),
                    (float*)(w + L.many_acc), (float*)(w + L.many_ml)};
-    if (L.few_items > 0x7FFFFFFFLL || L.many_items > 0x7FFFFFFFLL) return RADIX_ERR_UNSUPPORTED;
-    const dim3 few((unsigned)L.few_items), many((unsigned)L.many_items), block(256);
-    const int join_rows = L.many ? MANY_ROWS : L.few_rows;
-    const dim3 join((unsigned)(L.units > 1024 ? 1024 : L.units), (unsigned)ceil_div(join_rows, 4));
-    if (dtype == RADIX_F32) {
-        if (c.head_dim <= 64)
-            hipLaunchKernelGGL((paged_few_kernel<FewTileF32<1>, 1>), few, block, 0, stream, a, (const float*)q, (float*)out, status);
-        else
-            hipLaunchKernelGGL((paged_few_kernel<FewTileF32<2>, 1>), few, block, 0, stream, a, (const float*)q, (float*)out, status);
-        hipLaunchKernelGGL(paged_join_kernel<float>, join, block, 0, stream, a, (float*)out);
-        return RADIX_OK;
-    }
-#define RADIX_PAGED(DT)                                                                                                                  \
-    do {                                                                                                                                 \
-        typedef Op<DT>::T T;                                                                                                             \
-        if (L.few_rows == 16) hipLaunchKernelGGL((paged_few_kernel<FewTile<DT, 1>, 1>), few, block, 0, stream, a, (const T*)q, (T*)out, status); \
-        else hipLaunchKernelGGL((paged_few_kernel<FewTile<DT, 2>, 2>), few, block, 0, stream, a, (const T*)q, (T*)out, status);           \
-        if (L.many) hipLaunchKernelGGL(paged_many_kernel<DT>, many, block, 0, stream, a, (const T*)q, (T*)out, status);                   \
-        hipLaunchKernelGGL(paged_join_kernel<T>, join, block, 0, stream, a, (T*)out);                                                     \
+    if (L.items > 0x7FFFFFFFLL) return RADIX_ERR_UNSUPPORTED;
+    const JoinArgs j = {cu, a.plan + L.join, a.plan + L.splits, a.plan + L.slot, a.few_acc, a.few_ml, a.many_acc, a.many_ml, s.B, s.N, s.max_new,
+                        c.n_kv_heads, s.n_q_heads / c.n_kv_heads, c.head_dim, L.few_rows, (int)L.few_slots, (int)L.many_slots, (int)s.out_stride,
+                        L.many != 0};
+    const dim3 grid((unsigned)L.items), block(256), join((unsigned)(L.joins > 1024 ? 1024 : L.joins));
+#define RADIX_PAGED(KERNEL, T)                                                                                       \
+    do {                                                                                                             \
+        hipLaunchKernelGGL((KERNEL), grid, block, 0, stream, a, (const T*)q, (T*)out, status);                       \
+        hipLaunchKernelGGL((paged_join_kernel<T>), join, block, 0, stream, j, (T*)out);                              \
     } while (0)
-    if (dtype == RADIX_BF16) RADIX_PAGED(RADIX_BF16); else RADIX_PAGED(RADIX_F16);
+#define RADIX_PAGED_16(DT)                                                                                           \
+    do {                                                                                                             \
+        typedef Op<DT>::T T;                                                                                         \
+        if (L.many) RADIX_PAGED(paged_mixed_kernel<DT>, T);                                                          \
+        else if (L.few_rows == 16) RADIX_PAGED((paged_few_kernel<FewTile<DT, 1>, 1>), T);                            \
+        else RADIX_PAGED((paged_few_kernel<FewTile<DT, 2>, 2>), T);                                                  \
+    } while (0)
+    if (dtype == RADIX_F32) {
+        if (c.head_dim <= 64) RADIX_PAGED((paged_few_kernel<FewTileF32<1>, 1>), float);
+        else RADIX_PAGED((paged_few_kernel<FewTileF32<2>, 1>), float);
+    } else if (dtype == RADIX_BF16) RADIX_PAGED_16(RADIX_BF16);
+    else RADIX_PAGED_16(RADIX_F16);
+#undef RADIX_PAGED_16
 #undef RADIX_PAGED
     return RADIX_OK;
 }
