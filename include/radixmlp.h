@@ -312,7 +312,7 @@ int radix_index_select_rows(const void* src, int32_t n_src_rows, const int32_t* 
  *   pages       [n_layers][n_pages][2][n_kv_heads][page_size][head_dim] in `dtype`: keys (0) and values (1), 16-byte
  *               aligned, radix_cache_bytes bytes.  A cache for a model has its layers, kv heads, head size and
  *               compute_dtype.  Shapes: page_size 16, 32, 64, 128 or 256; head_dim 128 with 16-bit types, a multiple of
- *               4 up to 128 with RADIX_F32.
+ *               4 up to 128 with RADIX_F32; a page of a layer below 2^31 bytes.
  *   page_refs   int32[n_pages]  number of table entries that hold the page; 0 = free
  *   page_table  int32[max_seqs][max_pages]  entry i of a row: the page with positions i * page_size ..; -1 = none
  *   seq_lens    int32[max_seqs]  positions in the cache.  A row of length n holds its pages in its first
@@ -413,8 +413,8 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  *                 scores are scaled by 1 / sqrt(head_dim)
  *   max_new       >= tokens of any sequence of the call (host value, sizes the grid)
  *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new), 256-byte aligned
- * past[b] < 0: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position are not
- * read; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).
+ * past[b] < 0: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position have
+ * no influence; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).
  * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values.
  * A sequence whose range is not in [0, N) or longer than max_new (RADIX_ERR_BAD_CU_SEQLENS) is left out; a slot out of
  * range (RADIX_ERR_BAD_SLOT) or more positions than a table row holds (RADIX_ERR_BAD_PAGE): zeros; a table entry that is no

@@ -335,9 +335,9 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheView c, const int3
         for (; v + 7 * 64 < vecs; v += 8 * 64) {
             u32x4 x[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = s[v + 64 * k];
+            for (int k = 0; k < 8; ++k) x[k] = __builtin_nontemporal_load(s + v + 64 * k);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) d[v + 64 * k] = x[k];
+            for (int k = 0; k < 8; ++k) __builtin_nontemporal_store(x[k], d + v + 64 * k);
         }
         for (; v < vecs; v += 64) d[v] = s[v];
     }

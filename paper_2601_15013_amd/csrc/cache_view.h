@@ -21,6 +21,7 @@ static inline int cache_shape(const radix_cache* c, CacheView* v) {
           shift, c->max_seqs, c->max_pages, 0, 0, 0};
     v->piece_bytes = (size_t)c->page_size * c->head_dim * (c->dtype == RADIX_F32 ? 4 : 2);
     v->page_bytes = 2 * (size_t)c->n_kv_heads * v->piece_bytes;
+    if (v->page_bytes > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
     v->layer_bytes = (size_t)c->n_pages * v->page_bytes;
     return RADIX_OK;
 }

@@ -274,7 +274,7 @@ struct PagedShape {
 struct PagedLayout {
     size_t item_few, item_many, join, slot, splits;                              // int32 words
     size_t few_acc, few_ml, many_acc, many_ml, total;                            // bytes
-    int few_rows, few_tile, many;        // rows of a block / keys of a tile for few rows; whether there can be blocks of many rows
+    int few_rows, few_tile, few_target, many;        // rows of a block / keys of a tile for few rows; whether there can be blocks of many rows
     long long items, few_slots, many_slots, joins;                           // upper bounds
 };
 PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s);

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int v = base + u * 256 + (int)threadIdx.x;
-            next[u] = xv[v < v1 ? v : v1 - 1];
+            next[u] = __builtin_nontemporal_load(xv + (v < v1 ? v : v1 - 1));
         }
     };
     if (v0 < v1) fetch(v0);
