@@ -24,12 +24,26 @@ __device__ __forceinline__ void wave_order() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
-// Larger for larger x; equal values: larger for the lower id; a NaN comes last.  Never 0.
-__device__ __forceinline__ u64 key_of(float x, int id) {
+// Larger for larger x; a NaN comes last.
+__device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t b = __float_as_uint(x + 0.0f);            // -0 counts as 0
-    uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
-    if (x != x) o = 0;
-    return ((u64)o << 32) | (0xFFFFFFFFu - (uint32_t)id);
+    const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
+    return x != x ? 0u : o;
+}
+// Equal values: larger for the lower id.  Never 0.
+__device__ __forceinline__ u64 key_of(float x, int id) { return ((u64)ordered(x) << 32) | (0xFFFFFFFFu - (uint32_t)id); }
+// A bound (an ordered value) that at least k lanes' x reach, so that no value below it is among the k largest; the largest one whose lower
+// 16 bits are 0.  0 where fewer than k lanes have one above -inf.
+__device__ __forceinline__ uint32_t bound_of(float x, int k) {
+    const uint32_t o = ordered(x);
+    uint32_t bound = 0;
+    if (__popcll(__ballot(x > -INFINITY)) < k) return 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t next = bound | (1u << bit);
+        if (__popcll(__ballot(o >= next)) >= k) bound = next;
+    }
+    return bound;
 }
 __device__ __forceinline__ float value_of(u64 key) {
     const uint32_t o = (uint32_t)(key >> 32);
@@ -93,15 +107,23 @@ struct Answer {
     float *logprobs, *entropy, *top_logprobs;
     int32_t *top_ids, *status;
 };
+// The logits of a row's given tokens, one a lane, asked for before the rest of the row is through.
+struct Given { int token; float x; };
+template <typename T> __device__ __forceinline__ Given ask_given(const Answer& a, const T* x, size_t row, int j) {
+    Given g = {-1, 0.f};
+    if (j < a.n_given) g.token = a.given[row * a.n_given + j];
+    if (g.token >= 0 && g.token < a.vocab) g.x = to_f32<T>(x[g.token]);
+    return g;
+}
 // The row's results from its statistics and its sorted list, by one wavefront.
 template <typename T>
-__device__ __forceinline__ void answer(const Answer& a, const T* x, size_t row, Stat st, const u64* list, int n, int lane) {
+__device__ __forceinline__ void answer(const Answer& a, const T* x, size_t row, Stat st, const u64* list, int n, Given g, int lane) {
     const float ls = st.s > 0.f ? logf(st.s) : NAN;           // no finite logit, or a NaN or +inf among them: no distribution
     for (int j = lane; j < a.n_given; j += 64) {
-        const int t = a.given[row * a.n_given + j];
-        float y = 0.f;                                        // t < 0: no token
-        if (t >= a.vocab) { set_status(a.status, RADIX_ERR_BAD_TOKEN); y = NAN; }
-        else if (t >= 0) y = (to_f32<T>(x[t]) - st.m) - ls;
+        if (j >= 64) g = ask_given<T>(a, x, row, j);
+        float y = 0.f;                                        // token < 0: none
+        if (g.token >= a.vocab) { set_status(a.status, RADIX_ERR_BAD_TOKEN); y = NAN; }
+        else if (g.token >= 0) y = (g.x - st.m) - ls;
         a.logprobs[row * a.n_given + j] = y;
     }
     if (lane == 0 && a.entropy) a.entropy[row] = ls - st.t / st.s;
@@ -113,7 +135,7 @@ __device__ __forceinline__ void answer(const Answer& a, const T* x, size_t row, 
 }
 
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict__ logits, size_t ld, int splits, Answer a,
+__global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict__ logits, size_t ld, int splits, int per, Answer a,
                                                              Stat* __restrict__ part_stat, u64* __restrict__ part_list) {
     constexpr int V = 16 / sizeof(T), U = 16 / V;             // elements of a vector, vectors of a thread per turn
     typedef __attribute__((ext_vector_type(V))) T Vec;
@@ -129,8 +151,7 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
     const int head = to_line < a.vocab ? to_line : a.vocab;
     const int vecs = (a.vocab - head) / V, tail = a.vocab - head - vecs * V;
     const Vec* xv = reinterpret_cast<const Vec*>(x + head);
-    const int per = (vecs + splits - 1) / splits;
-    const int v0 = split * per < vecs ? split * per : vecs, v1 = v0 + per < vecs ? v0 + per : vecs;
+    const int v0 = split * per * U * 256 < vecs ? split * per * U * 256 : vecs, v1 = v0 + per * U * 256 < vecs ? v0 + per * U * 256 : vecs;
     u64* list = lists[wave];
     int n = 0;                                                // entries of this wavefront's list
     float thr = 0.f;
@@ -152,29 +173,19 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
         const float use = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int u = 0; u < NE; ++u) {
-            float d = e[u] - use;
-            d = d < -1e4f ? -1e4f : d;                                          // -inf: no part in s, and 0 in t instead of -inf * 0
-            const float p = __builtin_amdgcn_exp2f(d * LOG2E);
+            const float d = e[u] - use, p = __builtin_amdgcn_exp2f(d * LOG2E);
             s += p;
-            t = fmaf(d, p, t);
+            t = fmaf(fmaxf(d, -1e4f), p, t);                                    // 0 for d = -inf, where p is 0
         }
         if constexpr (TOP) {
             if (full && !__any(top > thr)) return;
-            if (!full && n == 0) {                            // a first bound: the k-th best of the lanes' maxima
-                u64 best = 0;
+            if (!full && n == 0) {                            // a first bound, from the lanes' maxima
+                const uint32_t bound = bound_of(top, a.k);
 #pragma unroll
                 for (int u = 0; u < NE; ++u) {
-                    const u64 key = valid(u) ? key_of(e[u], id(u)) : 0;
-                    best = key > best ? key : best;
-                }
-                const int rank = rank_of(best, 64);
-                const u64 at = __ballot(rank == a.k - 1 && best != 0);
-                const u64 bound = at ? read_lane(best, __ffsll((long long)at) - 1) : 1;
-#pragma unroll
-                for (int u = 0; u < NE; ++u) {
-                    const u64 key = valid(u) ? key_of(e[u], id(u)) : 0;
-                    const u64 in = __ballot(key >= bound);
-                    if (key >= bound) list[n + __popcll(in & ((1ull << lane) - 1ull))] = key;
+                    const bool keep = valid(u) && ordered(e[u]) >= bound;
+                    const u64 in = __ballot(keep);
+                    if (keep) list[n + __popcll(in & ((1ull << lane) - 1ull))] = key_of(e[u], id(u));
                     n += __popcll(in);
                 }
             } else {
@@ -211,19 +222,20 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
         }
     };
     if (v0 < v1) fetch(v0);
-    for (int base = v0; base < v1; base += U * 256) {
+    auto turn = [&](int base, auto whole) {                   // whole: every lane's vectors are in the range
         float e[16];
+        auto in = [&](int u) { return decltype(whole)::value != 0 || base + u / V * 256 + (int)threadIdx.x < v1; };
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float y = to_f32<T>(next[u][i]);
-                e[u * V + i] = base + u * 256 + (int)threadIdx.x < v1 ? y : -INFINITY;
-            }
+        for (int u = 0; u < 16; ++u) {
+            const float y = to_f32<T>(next[u / V][u % V]);
+            e[u] = in(u) ? y : -INFINITY;
+        }
         if (base + U * 256 < v1) fetch(base + U * 256);
-        take(Count<16>{}, e, [&](int u) { return base + u / V * 256 + (int)threadIdx.x < v1; },
-             [&](int u) { return head + (base + u / V * 256 + (int)threadIdx.x) * V + u % V; });
-    }
+        take(Count<16>{}, e, in, [&](int u) { return head + (base + u / V * 256 + (int)threadIdx.x) * V + u % V; });
+    };
+    int base = v0;
+    for (; base + U * 256 <= v1; base += U * 256) turn(base, Count<1>{});
+    if (base < v1) turn(base, Count<0>{});
     if (edges && tail > 0) take_edge(head + vecs * V, tail);
 
     // ---- the wavefront's, then the workgroup's: lanes and wavefronts are joined in a fixed tree
@@ -248,7 +260,7 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
         n = cut_list(list, n, a.k, lane);
     }
     if (splits == 1) {
-        answer<T>(a, x, row, st, list, n, lane);
+        answer<T>(a, x, row, st, list, n, ask_given<T>(a, x, row, lane), lane);
     } else {
         const size_t at = row * splits + split;
         if (lane == 0) part_stat[at] = st;
@@ -262,6 +274,7 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(const T* __rest
     __shared__ u64 list[64 * 32];
     const int lane = threadIdx.x;
     const size_t row = blockIdx.x;
+    const Given g = ask_given<T>(a, logits + row * ld, row, lane);
     Stat st = {-INFINITY, 0.f, 0.f};                          // at most 64 splits: one a lane
     if (lane < splits) st = part_stat[row * splits + lane];
 #pragma unroll
@@ -272,25 +285,30 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(const T* __rest
     int n = 0;
     if (a.k > 0) {
         const int c = splits * a.k;
-        for (int i0 = 0; i0 < c; i0 += 64) {
-            const u64 key = i0 + lane < c ? part_list[row * c + i0 + lane] : 0;
-            const u64 in = __ballot(key != 0);
-            if (key != 0) list[n + __popcll(in & ((1ull << lane) - 1ull))] = key;
-            n += __popcll(in);
+        for (int i0 = 0; i0 < c; i0 += 256) {
+            u64 key[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) key[u] = i0 + 64 * u + lane < c ? part_list[row * c + i0 + 64 * u + lane] : 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const u64 in = __ballot(key[u] != 0);
+                if (key[u] != 0) list[n + __popcll(in & ((1ull << lane) - 1ull))] = key[u];
+                n += __popcll(in);
+            }
         }
         wave_order();
         n = cut_list(list, n, a.k, lane);
     }
-    answer<T>(a, logits + row * ld, row, st, list, n, lane);
+    answer<T>(a, logits + row * ld, row, st, list, n, g, lane);
 }
 
 }  // namespace
 
-// Workgroups for the chip (four a CU), no more than 64 a row, each with at least two turns' worth of vectors.
-int token_logprobs_splits(int n_rows, int vocab) {
-    const int by_rows = n_rows > 0 ? 1024 / n_rows : 1, by_length = vocab / 4096;
-    int n = by_rows < by_length ? by_rows : by_length;
-    return n < 1 ? 1 : (n > 64 ? 64 : n);
+// Turns (of 4096 elements) of a workgroup, and workgroups of a row: four a CU for the whole chip, no more than 64 a row.
+static void shape_of(int n_rows, int vocab, int* per, int* splits) {
+    const int turns = vocab / 4096 + (vocab % 4096 != 0), wanted = n_rows < 1024 ? 1024 / n_rows : 1, most = wanted < 64 ? wanted : 64;
+    *per = (turns + most - 1) / most;
+    *splits = (turns + *per - 1) / *per;
 }
 
 size_t token_logprobs_ws_bytes(int n_rows, int k) {
@@ -301,15 +319,16 @@ size_t token_logprobs_ws_bytes(int n_rows, int k) {
 void launch_token_logprobs(const void* logits, int dtype, size_t ld, int n_rows, int vocab, const int32_t* given, int n_given, int k,
                            float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs, void* ws, int32_t* status,
                            hipStream_t stream) {
-    const int splits = token_logprobs_splits(n_rows, vocab);
+    int per, splits;
+    shape_of(n_rows, vocab, &per, &splits);
     const Answer a = {given, n_given, k, vocab, logprobs, entropy, top_logprobs, top_ids, status};
     Stat* ps = (Stat*)ws;
     u64* pl = (u64*)((char*)ws + align_up((size_t)n_rows * splits * sizeof(Stat), 256));
     const dim3 grid((unsigned)n_rows * (unsigned)splits);
 #define RADIX_LOGPROBS(T)                                                                                                              \
     do {                                                                                                                               \
-        if (k > 0) hipLaunchKernelGGL((token_logprobs_kernel<T, true>), grid, dim3(256), 0, stream, (const T*)logits, ld, splits, a, ps, pl); \
-        else hipLaunchKernelGGL((token_logprobs_kernel<T, false>), grid, dim3(256), 0, stream, (const T*)logits, ld, splits, a, ps, pl);  \
+        if (k > 0) hipLaunchKernelGGL((token_logprobs_kernel<T, true>), grid, dim3(256), 0, stream, (const T*)logits, ld, splits, per, a, ps, pl); \
+        else hipLaunchKernelGGL((token_logprobs_kernel<T, false>), grid, dim3(256), 0, stream, (const T*)logits, ld, splits, per, a, ps, pl);  \
         if (splits > 1)                                                                                                                \
             hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3((unsigned)n_rows), dim3(64), 0, stream, (const T*)logits, ld, splits, a, ps, pl); \
     } while (0)
