@@ -398,12 +398,20 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, int laye
     const size_t row_bytes = c.piece_bytes / c.page_size;
     const int row_vecs = (int)(row_bytes / 16), vecs = c.n_kv_heads * row_vecs;
     char* base = c.pages + (size_t)layer * c.layer_bytes + (size_t)page * c.page_bytes + (size_t)(p % c.page_size) * row_bytes;
-    const uint4* ks = reinterpret_cast<const uint4*>(k + (size_t)i * k_stride);
-    const uint4* vs = reinterpret_cast<const uint4*>(v + (size_t)i * v_stride);
-    for (int e = lane; e < 2 * vecs; e += 64) {
-        const int x = e < vecs ? e : e - vecs;
-        const int piece = (e < vecs ? 0 : c.n_kv_heads) + x / row_vecs;
-        *reinterpret_cast<uint4*>(base + (size_t)piece * c.piece_bytes + (size_t)(x % row_vecs) * 16) = e < vecs ? ks[x] : vs[x];
+    const u32x4* ks = reinterpret_cast<const u32x4*>(k + (size_t)i * k_stride);
+    const u32x4* vs = reinterpret_cast<const u32x4*>(v + (size_t)i * v_stride);
+    for (int e0 = lane; e0 < 2 * vecs; e0 += 4 * 64) {      // four vectors in flight
+        u32x4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = e0 + 64 * u;
+            if (e < 2 * vecs) y[u] = __builtin_nontemporal_load(e < vecs ? ks + e : vs + (e - vecs));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = e0 + 64 * u, x = e < vecs ? e : e - vecs, piece = (e < vecs ? 0 : c.n_kv_heads) + x / row_vecs;
+            if (e < 2 * vecs) *reinterpret_cast<u32x4*>(base + (size_t)piece * c.piece_bytes + (size_t)(x % row_vecs) * 16) = y[u];
+        }
     }
 }
 
