@@ -288,6 +288,12 @@ __device__ __forceinline__ const char* page_at(const CacheView& c, const char* b
     return base + (uint64_t)checked_page(c, p, bad) * (uint32_t)c.page_bytes;        // pages are smaller than 2^31 bytes
 }
 
+// Tiles are dealt to the parts evenly, the first ones one more where it does not come out.
+__device__ __forceinline__ int part_begin(int tiles, int part, int parts) {
+    const int per = (int)((unsigned)tiles / (unsigned)parts), more = tiles - per * parts;
+    return part * per + min(part, more);
+}
+
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 
 // ------------------------------------------------------------------ few rows
@@ -471,7 +477,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
     // the item's tiles: its share of those up to the last position that a row of the block sees
     const int last_row = min(row0 + ROWS, rows) - 1;
     const int tiles = sq.len > 0 ? (past + last_row / group) / Tile::KEYS + 1 : 0;
-    const int t0 = (int)((long long)tiles * w.split / w.splits), t1 = (int)((long long)tiles * (w.split + 1) / w.splits);
+    const int t0 = part_begin(tiles, w.split, w.splits), t1 = part_begin(tiles, w.split + 1, w.splits);
     const int32_t* table = a.c.table + (size_t)sq.row * a.c.max_pages;
     const char* base = a.c.pages + (size_t)a.layer * a.c.layer_bytes + (size_t)w.kvh * a.c.piece_bytes;
 
@@ -617,7 +623,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedItem& w
     const int group = a.s.n_q_heads / a.c.n_kv_heads, rows = sq.n * group;
     const int row0 = w.blk * MANY_ROWS, last_row = min(row0 + MANY_ROWS, rows) - 1;
     const int tiles = sq.len > 0 ? (past + last_row / group) / BKV + 1 : 0;
-    const int t0 = (int)((long long)tiles * w.split / w.splits), t1 = (int)((long long)tiles * (w.split + 1) / w.splits);
+    const int t0 = part_begin(tiles, w.split, w.splits), t1 = part_begin(tiles, w.split + 1, w.splits);
     const int32_t* table = a.c.table + (size_t)sq.row * a.c.max_pages;
     const char* base = a.c.pages + (size_t)a.layer * a.c.layer_bytes + (size_t)w.kvh * a.c.piece_bytes;
     const int last = sq.len - 1;
@@ -908,7 +914,8 @@ PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s) {
     L.few_target = few_blocks * kv < FEW_TARGET_EVEN / 2 ? FEW_TARGET_EVEN : FEW_TARGET;
     L.few_slots = 2 * FEW_TARGET;
     L.many_slots = L.many ? MANY_TARGET : 0;
-    L.joins = N * s.n_q_heads;                               // entries of the join: a row at the least
+    // entries of the join: a row at the least; none where a row of the table holds no more than one part (few_length, many_length)
+    L.joins = (long long)c.max_pages * c.page_size <= 256 ? 0 : N * s.n_q_heads;
     size_t w = 64;
     auto words = [&](size_t n) { const size_t o = w; w += n; return o; };
     L.item_few = words((size_t)B + 1);
@@ -947,7 +954,7 @@ int launch_paged_attention(const CacheView& c, int dtype, int layer, const Paged
 #define RADIX_PAGED(KERNEL, T)                                                                                       \
     do {                                                                                                             \
         hipLaunchKernelGGL((KERNEL), grid, block, 0, stream, a, (const T*)q, (T*)out, status);                       \
-        hipLaunchKernelGGL((paged_join_kernel<T>), join, block, 0, stream, j, (T*)out);                              \
+        if (L.joins > 0) hipLaunchKernelGGL((paged_join_kernel<T>), join, block, 0, stream, j, (T*)out);                              \
     } while (0)
 #define RADIX_PAGED_16(DT)                                                                                           \
     do {                                                                                                             \

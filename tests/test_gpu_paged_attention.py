@@ -177,6 +177,18 @@ def test_many_sequences(dtype, hd):
     check(past, news, 2, 1, hd, 16, dtype)
 
 
+@pytest.mark.parametrize("B", [63, 64, 65, 128, 200, 256, 257])
+@pytest.mark.parametrize("dtype,most", [("bf16", 1), ("bf16", 100), ("f32", 3)])
+def test_numbers_of_sequences_around_the_plan(B, dtype, most):
+    # a few long ones, which are split, anywhere among short and empty ones
+    rng = random.Random(B)
+    news = [rng.choice([0, 1, 1, most]) for _ in range(B)]
+    past = [rng.choice([0, 3, 20, 20, 20, 900 if rng.random() < 0.2 else 40]) for _ in news]
+    past[-1], news[-1] = 1500, 1
+    past[B // 2], news[B // 2] = 2500, most
+    check(past, news, 4, 2, 128 if dtype != "f32" else 32, 32, dtype)
+
+
 def test_results_do_not_depend_on_the_run():
     cache = CU.random_cache(5, [4000, 900, 30], 2, 128, 32, "bf16")
     q = queries(6, 3, 8, 128, "bf16")
