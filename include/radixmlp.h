@@ -325,6 +325,7 @@ int radix_index_select_rows(const void* src, int32_t n_src_rows, const int32_t* 
  * all or nothing: on an error nothing has changed.
  */
 #define RADIX_CACHE_MAX_LIST 65535
+#define RADIX_CACHE_MAX_SLOTS 262144     /* max_seqs; n_pages may be 2^28 */
 typedef struct radix_cache {
     int32_t n_layers;
     int32_t n_kv_heads;

@@ -5,7 +5,7 @@
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-static size_t page_ws_bytes(const CacheView& v, size_t n) { return align_up(page_ws_layout(v.max_seqs, v.n_pages, n).total * 4, 256); }
+static size_t page_ws_bytes(const CacheView& v, size_t n) { return align_up(page_ws_layout(v.n_pages, n).total * 4, 256); }
 
 // What the calls with a list of n entries and a workspace share.
 static int check_page_call(const radix_cache* cache, int32_t n, const void* ws, size_t ws_bytes, CacheView* v) {

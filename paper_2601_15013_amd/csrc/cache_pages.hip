@@ -53,6 +53,18 @@ __device__ __forceinline__ int number_pages(const int32_t* __restrict__ refs, in
     return found < want ? found : want;
 }
 
+// Slots that a call has met, a bit each, in LDS (in global memory every look was a round trip of a microsecond).
+struct Marks {
+    uint32_t bits[CACHE_MAX_SLOTS / 32];
+    __device__ __forceinline__ void clear(int slots) {
+        for (int i = threadIdx.x; i < (slots + 31) / 32; i += PT) bits[i] = 0;
+    }
+    __device__ __forceinline__ bool set(int slot) {         // whether it was set before
+        return atomicOr(&bits[slot >> 5], 1u << (slot & 31)) >> (slot & 31) & 1u;
+    }
+    __device__ __forceinline__ bool has(int slot) const { return bits[slot >> 5] >> (slot & 31) & 1u; }
+};
+
 __device__ __forceinline__ int pages_of(int tokens, int page_size) { return (tokens + page_size - 1) / page_size; }
 
 // The sequence of entry r of a list that `first` (exclusive sums, n + 1 entries) describes.
@@ -74,13 +86,11 @@ __global__ __launch_bounds__(PT) void cache_extend_kernel(CacheView c, const int
     __shared__ long long part[PT / 64];
     __shared__ int cnt[2][64];
     __shared__ int bad, n_moves;
+    __shared__ Marks met;
     const int tid = threadIdx.x, P = c.page_size;
-    int32_t *mark = ws + L.mark, *list = ws + L.list, *first = ws + L.first, *shared = ws + L.shared;
+    int32_t *list = ws + L.list, *first = ws + L.first, *shared = ws + L.shared;
     if (tid == 0) { bad = gate ? *gate : 0; n_moves = 0; }
-    for (int b = tid; b < B; b += PT) {
-        const int s = slots ? slots[b] : b;
-        if (s >= 0 && s < c.max_seqs) atomicExch(&mark[s], 0);
-    }
+    met.clear(c.max_seqs);
     __syncthreads();
     long long run = 0;
     for (int b0 = 0; b0 < B; b0 += PT) {
@@ -90,7 +100,7 @@ __global__ __launch_bounds__(PT) void cache_extend_kernel(CacheView c, const int
             const int s = slots ? slots[b] : b;
             const long long from = cu[b], to = cu[b + 1], n = to - from;
             if (from < 0 || n < 0 || (b == 0 && from != 0)) err = RADIX_ERR_BAD_CU_SEQLENS;
-            else if (s < 0 || s >= c.max_seqs || atomicAdd(&mark[s], 1) != 0) err = RADIX_ERR_BAD_SLOT;
+            else if (s < 0 || s >= c.max_seqs || met.set(s)) err = RADIX_ERR_BAD_SLOT;
             else {
                 const int len = c.lens[s];
                 if (len < 0 || len > (long long)c.max_pages * P) err = RADIX_ERR_BAD_PAGE;
@@ -159,14 +169,13 @@ __global__ __launch_bounds__(PT) void cache_fork_kernel(CacheView c, const int32
     __shared__ long long part[PT / 64];
     __shared__ int cnt[2][64];
     __shared__ int bad;
+    __shared__ Marks is_child, is_parent;
     const int tid = threadIdx.x, P = c.page_size;
-    int32_t *mark = ws + L.mark, *list = ws + L.list, *first = ws + L.first;
+    int32_t *list = ws + L.list, *first = ws + L.first;
     auto ok_slot = [&](int s) { return s >= 0 && s < c.max_seqs; };
     if (tid == 0) bad = 0;
-    for (int i = tid; i < n; i += PT) {
-        if (ok_slot(parents[i])) atomicExch(&mark[parents[i]], 0);
-        if (ok_slot(children[i])) atomicExch(&mark[children[i]], 0);
-    }
+    is_child.clear(c.max_seqs);
+    is_parent.clear(c.max_seqs);
     __syncthreads();
     long long run = 0;
     for (int i0 = 0; i0 < n; i0 += PT) {
@@ -176,8 +185,8 @@ __global__ __launch_bounds__(PT) void cache_fork_kernel(CacheView c, const int32
             const int p = parents[i], s = children[i];
             if (!ok_slot(p) || !ok_slot(s)) err = RADIX_ERR_BAD_SLOT;
             else {
-                if (atomicOr(&mark[s], 1) & 1) err = RADIX_ERR_BAD_SLOT;            // the same child twice
-                atomicOr(&mark[p], 2);
+                if (is_child.set(s)) err = RADIX_ERR_BAD_SLOT;                      // the same child twice
+                is_parent.set(p);
                 const int len = c.lens[p];
                 if (c.lens[s] != 0) err = RADIX_ERR_BAD_SLOT;                       // the child holds something
                 else if (len < 0 || len > (long long)c.max_pages * P) err = RADIX_ERR_BAD_PAGE;
@@ -196,7 +205,7 @@ __global__ __launch_bounds__(PT) void cache_fork_kernel(CacheView c, const int32
     if (tid == 0) first[n] = (int)run;
     __syncthreads();
     for (int i = tid; i < n; i += PT)                                               // a child that is a parent, too
-        if (ok_slot(children[i]) && (atomicOr(&mark[children[i]], 0) & 2)) atomicMin(&bad, (int)RADIX_ERR_BAD_SLOT);
+        if (ok_slot(children[i]) && is_parent.has(children[i])) atomicMin(&bad, (int)RADIX_ERR_BAD_SLOT);
     __syncthreads();
     if (bad == 0 && run <= c.n_pages) {
         const int got = number_pages(c.refs, 0, c.n_pages, (int)run, cnt, [](int r) { return r == 0; }, [&](int p, int k) { list[k] = p; });
@@ -444,7 +453,7 @@ void launch_cache_reset(const CacheView& c, hipStream_t stream) {
 
 void launch_cache_extend(const CacheView& c, const int32_t* slots, const int32_t* cu, int B, int limit, int32_t* past, int32_t* ws,
                          const int32_t* gate, int32_t* status, hipStream_t stream) {
-    const PageWs L = page_ws_layout(c.max_seqs, c.n_pages, B);
+    const PageWs L = page_ws_layout(c.n_pages, B);
     hipLaunchKernelGGL(cache_extend_kernel, dim3(1), dim3(PT), 0, stream, c, slots, cu, B, limit, past, ws, L, gate, status);
     hipLaunchKernelGGL(cache_move_kernel<TABLE_NONE>, dim3(move_blocks(c, B)), dim3(256), 0, stream, c, ws + L.src, ws + L.dst, ws + L.rows,
                        ws, 0, nullptr, nullptr, nullptr, status);
@@ -452,7 +461,7 @@ void launch_cache_extend(const CacheView& c, const int32_t* slots, const int32_t
 
 void launch_cache_fork(const CacheView& c, const int32_t* parents, const int32_t* children, int n, int32_t* ws, int32_t* status,
                        hipStream_t stream) {
-    const PageWs L = page_ws_layout(c.max_seqs, c.n_pages, n);
+    const PageWs L = page_ws_layout(c.n_pages, n);
     hipLaunchKernelGGL(cache_fork_kernel, dim3(1), dim3(PT), 0, stream, c, parents, children, n, ws, L, status);
     hipLaunchKernelGGL(cache_move_kernel<TABLE_FORK>, dim3(move_blocks(c, n) + (unsigned)n), dim3(256), 0, stream, c, ws + L.src, ws + L.dst,
                        ws + L.rows, ws, n, parents, children, nullptr, status);
@@ -463,7 +472,7 @@ void launch_cache_free(const CacheView& c, const int32_t* slots, const int32_t* 
 }
 
 void launch_cache_compact(const CacheView& c, int32_t* n_used, int32_t* ws, int32_t* status, hipStream_t stream) {
-    const PageWs L = page_ws_layout(c.max_seqs, c.n_pages, 0);
+    const PageWs L = page_ws_layout(c.n_pages, 0);
     hipLaunchKernelGGL(cache_compact_kernel, dim3(1), dim3(PT), 0, stream, c, n_used, ws, L);
     const size_t entries = (size_t)c.max_seqs * c.max_pages;
     const unsigned tb = (unsigned)(entries / 2048 > 1024 ? 1024 : entries / 2048 + 1);
@@ -473,7 +482,7 @@ void launch_cache_compact(const CacheView& c, int32_t* n_used, int32_t* ws, int3
 
 void launch_cache_copy(const CacheView& c, const int32_t* src, const int32_t* dst, int n, int32_t* ws, int32_t* status,
                        hipStream_t stream) {
-    const PageWs L = page_ws_layout(c.max_seqs, c.n_pages, 0);
+    const PageWs L = page_ws_layout(c.n_pages, 0);
     hipLaunchKernelGGL(cache_copy_check_kernel, dim3(1), dim3(PT), 0, stream, c, src, dst, n, ws, L, status);
     hipLaunchKernelGGL(cache_move_kernel<TABLE_NONE>, dim3(move_blocks(c, n)), dim3(256), 0, stream, c, src, dst, nullptr, ws, 0, nullptr,
                        nullptr, nullptr, status);

@@ -14,7 +14,7 @@ static inline int cache_shape(const radix_cache* c, CacheView* v) {
     if (c->dtype == RADIX_F32 ? (c->head_dim % 4 != 0 || c->head_dim > 128) : c->head_dim != 128) return RADIX_ERR_UNSUPPORTED;
     if (c->n_kv_heads > 65535 || c->n_layers > 65535) return RADIX_ERR_UNSUPPORTED;
     if ((int64_t)c->max_pages * c->page_size > INT32_MAX) return RADIX_ERR_BAD_SIZE;          // positions are 32-bit
-    if (c->n_pages > (1 << 28) || c->max_seqs > (1 << 28)) return RADIX_ERR_UNSUPPORTED;
+    if (c->n_pages > (1 << 28) || c->max_seqs > RADIX_CACHE_MAX_SLOTS) return RADIX_ERR_UNSUPPORTED;
     int shift = 4;
     while ((1 << shift) < c->page_size) ++shift;
     *v = {(char*)c->pages, c->page_refs, c->page_table, c->seq_lens, c->n_layers, c->n_pages, c->n_kv_heads, c->head_dim, c->page_size,

@@ -225,17 +225,17 @@ struct CacheView {
     int n_layers, n_pages, n_kv_heads, head_dim, page_size, page_shift, max_seqs, max_pages;     // page_size = 1 << page_shift
     size_t piece_bytes, page_bytes, layer_bytes;
 };
+constexpr int CACHE_MAX_SLOTS = RADIX_CACHE_MAX_SLOTS;
 // Scratch of the page calls, in int32 words behind a header {number of moves, ...} of 64 words.
 struct PageWs {
-    uint32_t mark, map, list, src, dst, rows, first, shared;
+    uint32_t map, list, src, dst, rows, first, shared;
     size_t total;                        // below 2^32
 };
-static inline PageWs page_ws_layout(size_t max_seqs, size_t n_pages, size_t n) {
+static inline PageWs page_ws_layout(size_t n_pages, size_t n) {
     PageWs L;
     size_t off = 64;
     const size_t moves = n > n_pages ? n : n_pages;
     auto take = [&](size_t words) { const size_t o = off; off += words; return (uint32_t)o; };
-    L.mark = take(max_seqs);
     L.map = take(n_pages);
     L.list = take(n_pages);
     L.src = take(moves);

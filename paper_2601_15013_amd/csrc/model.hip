@@ -643,7 +643,7 @@ int extend_setup(const radix_model* model, const radix_cache* cache, int N, int 
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes ? bytes : 1, 256); return o; };
     L->past = take((size_t)B * 4);
     L->pos = take((size_t)N * 4);
-    L->page = take(page_ws_layout(v->max_seqs, v->n_pages, (size_t)B).total * 4);
+    L->page = take(page_ws_layout(v->n_pages, (size_t)B).total * 4);
     L->attn = take(P->total);
     L->total = off;
     return RADIX_OK;

@@ -29,7 +29,8 @@ def cache(**kw):
 BAD_SHAPES = [(dict(n_layers=0), BAD_SIZE), (dict(n_kv_heads=-1), BAD_SIZE), (dict(head_dim=0), BAD_SIZE), (dict(n_pages=0), BAD_SIZE),
               (dict(max_seqs=0), BAD_SIZE), (dict(max_pages=0), BAD_SIZE), (dict(dtype=3), UNSUPPORTED), (dict(page_size=8), UNSUPPORTED),
               (dict(page_size=48), UNSUPPORTED), (dict(page_size=512), UNSUPPORTED), (dict(head_dim=64), UNSUPPORTED),
-              (dict(dtype=0, head_dim=66), UNSUPPORTED), (dict(dtype=0, head_dim=132), UNSUPPORTED), (dict(max_pages=1 << 27), BAD_SIZE)]
+              (dict(dtype=0, head_dim=66), UNSUPPORTED), (dict(dtype=0, head_dim=132), UNSUPPORTED), (dict(max_pages=1 << 27), BAD_SIZE), (dict(max_seqs=262145), UNSUPPORTED),
+              (dict(n_pages=(1 << 28) + 1), UNSUPPORTED), (dict(n_kv_heads=65535, page_size=256), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_SHAPES)
