@@ -354,7 +354,8 @@ int radix_cache_reset(const radix_cache* cache, void* stream);
  * by that, the pages that it needs are taken, and past[b] becomes the length before.  radix_cache_append then stores the
  * tokens' keys and values layer by layer, radix_paged_attention attends to them.  A last page that is partly filled and
  * shared with another slot is replaced by a copy first.
- * Errors: RADIX_ERR_BAD_CU_SEQLENS (not 0 .. non-decreasing), RADIX_ERR_BAD_SLOT (out of range or listed twice),
+ * Errors: RADIX_ERR_BAD_CU_SEQLENS (not 0 .. non-decreasing), RADIX_ERR_BAD_SLOT (out of range or listed twice, entries
+ * without new tokens included),
  * RADIX_ERR_OUT_OF_PAGES (also: longer than max_pages * page_size), RADIX_ERR_BAD_PAGE (a length or an entry that cannot
  * be); then past[b] = -1 for all b, with which append stores nothing and attention gives zeros.
  */
@@ -400,7 +401,7 @@ int radix_cache_copy_pages(const radix_cache* cache, const int32_t* src, const i
  *                 lie in fused q | k | v rows), 16-byte aligned, strides multiples of 16 bytes
  *   cu_seqlens    int32[B+1]; rows from cu_seqlens[B] on belong to no sequence and are ignored
  * A position without a page (RADIX_ERR_BAD_PAGE), a slot out of range (RADIX_ERR_BAD_SLOT) or a range outside [0, N)
- * (RADIX_ERR_BAD_CU_SEQLENS): the token is left out and reported.
+ * (RADIX_ERR_BAD_CU_SEQLENS): the token is left out and reported.  N < 2^24.
  */
 int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                        const int32_t* cu_seqlens, const int32_t* past, const int32_t* slots, int32_t B, int32_t N,
@@ -419,7 +420,9 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values.
  * A sequence whose range is not in [0, N) or longer than max_new (RADIX_ERR_BAD_CU_SEQLENS) is left out; a slot out of
  * range (RADIX_ERR_BAD_SLOT) or more positions than a table row holds (RADIX_ERR_BAD_PAGE): zeros; a table entry that is no
- * page is read as page 0 (RADIX_ERR_BAD_PAGE).  N * n_q_heads < 2^31.
+ * page is read as page 0 (RADIX_ERR_BAD_PAGE).  Results are the same in every run; how a sequence's keys are split over workgroups,
+ * and with it the order of its sums, depends on the whole batch.  N * n_q_heads < 2^31; RADIX_ERR_UNSUPPORTED also where the batch
+ * would take 2^24 workgroups.
  */
 int radix_paged_attention_workspace_bytes(const radix_cache* cache, int32_t n_q_heads, int32_t max_N, int32_t max_B,
                                           int32_t max_new, size_t* bytes_out);
@@ -437,8 +440,9 @@ int radix_paged_attention(const radix_cache* cache, int32_t layer, const void* q
  *   ws            at least radix_extend_workspace_bytes(model, cache, N, B, max_new), 256-byte aligned
  * The cache holds keys, values and attention outputs in compute_dtype: a leading (hi, lo) layer (hilo_layers) keeps pairs for its
  * GEMM inputs only, not for q, k, v and the attention output.  A sequence may hold min(max_pages * page_size, max_pos) positions.
- * RADIX_ERR_BAD_CONFIG: the cache is not of the model's shape.  Device-data errors: radix_device_status(ws); where the cache could
- * not be extended (codes of radix_cache_extend) it has not changed, and out holds nothing of use.  Asynchronous on `stream`; can be
+ * RADIX_ERR_BAD_CONFIG: the cache is not of the model's shape.  Device-data errors (cu_seqlens has to end at N here): radix_device_status(ws); where the cache could
+ * not be extended (codes of radix_cache_extend) it has not changed, and out holds nothing of use; a token id out of range is clamped
+ * and reported (RADIX_ERR_BAD_TOKEN), and the cache has been extended.  Asynchronous on `stream`; can be
  * captured into a graph (replays extend the cache again).
  */
 int radix_extend_workspace_bytes(const radix_model* model, const radix_cache* cache, int32_t max_N, int32_t max_B, int32_t max_new,
@@ -456,7 +460,7 @@ int radix_extend_forward(const radix_model* model, const radix_cache* cache, con
  *                 logits by the lower id
  * Logits of -inf (tokens that are ruled out) have no part in the sums.  A row without a finite logit, or with a NaN or +inf, has
  * NaN for logprobs, entropy and top_logprobs; its ids are ordered as ever, a NaN last.  n_given, top_k may be 0 (pointers NULL then).
- * Sums are fp32; how a row is summed depends on n_rows and vocab only.
+ * Sums are fp32; how a row is summed depends on n_rows and vocab only.  n_rows < 2^24.
  */
 #define RADIX_MAX_TOP_K 32
 int radix_token_logprobs_workspace_bytes(int32_t max_rows, int32_t vocab, int32_t n_given, int32_t top_k, size_t* bytes_out);

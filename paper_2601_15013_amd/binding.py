@@ -389,9 +389,17 @@ def _list(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
     return _ptr(t)
 
 
-def _out(t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+def _new(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)         # written there, whatever stream it was made on
+    return t
+
+
+def _out(t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device,
+         stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _new(shape, dtype, device, stream)
     if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
     return t
@@ -449,7 +457,7 @@ def radix_cache_extend(cache: Cache, cu_seqlens: torch.Tensor, ws: torch.Tensor,
     """Room for the batch's new tokens; returns past[B], the lengths before (-1 everywhere if the call was refused)."""
     B = _i32(cu_seqlens, "cu_seqlens").numel() - 1
     _same_device(cache.device, cu_seqlens=cu_seqlens, ws=ws, slots=slots, past=past, status=status)
-    past = _out(past, "past", (B,), torch.int32, cache.device)
+    past = _out(past, "past", (B,), torch.int32, cache.device, stream)
     _launch("radix_cache_extend", cache.device, stream, cache.ref, _list(slots, "slots", B), _ptr(cu_seqlens), B, _ptr(past),
             _ptr(ws), ws.numel(), _status(status))
     return past
@@ -475,7 +483,7 @@ def radix_cache_compact(cache: Cache, ws: torch.Tensor, n_used: Optional[torch.T
                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Returns n_used[1]: used pages, which are pages 0 .. n_used - 1 now."""
     _same_device(cache.device, ws=ws, n_used=n_used, status=status)
-    n_used = _out(n_used, "n_used", (1,), torch.int32, cache.device)
+    n_used = _out(n_used, "n_used", (1,), torch.int32, cache.device, stream)
     _launch("radix_cache_compact", cache.device, stream, cache.ref, _ptr(n_used), _ptr(ws), ws.numel(), _status(status))
     return n_used
 
@@ -525,7 +533,7 @@ def radix_paged_attention(cache: Cache, layer: int, q: torch.Tensor, cu_seqlens:
     B, N = _i32(cu_seqlens, "cu_seqlens").numel() - 1, q.shape[0]
     qs = _token_rows(q, "q", cache)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _new(q.shape, q.dtype, q.device, stream)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
     os_ = _token_rows(out, "out", cache)
@@ -548,7 +556,7 @@ def radix_extend_forward(model: Model, cache: Cache, tok: torch.Tensor, cu_seqle
     """Forward of the new tokens tok[N] behind what the cache holds of their slots; returns the hidden states [N, d]."""
     N, B = _i32(tok, "tok").numel(), _i32(cu_seqlens, "cu_seqlens").numel() - 1
     _same_device(cache.device, tok=tok, cu_seqlens=cu_seqlens, ws=ws, slots=slots, out=out)
-    out = _out(out, "out", (N, model.cfg.d), torch.float32, cache.device)
+    out = _out(out, "out", (N, model.cfg.d), torch.float32, cache.device, stream)
     _launch("radix_extend_forward", cache.device, stream, model.handle, cache.ref, _ptr(tok), _ptr(cu_seqlens), _list(slots,
             "slots", B), B, N, max_new, _ptr(out), _ptr(ws), ws.numel())
     return out
@@ -568,10 +576,10 @@ def _given(given: Optional[torch.Tensor], n: int) -> int:
     return given.shape[1]
 
 
-def _answers(n: int, n_given: int, top_k: int, dev: torch.device) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
-    f = dict(dtype=torch.float32, device=dev)
-    return (torch.empty((n, n_given), **f), torch.empty(n, **f), torch.empty((n, top_k), dtype=torch.int32, device=dev),
-            torch.empty((n, top_k), **f))
+def _answers(n: int, n_given: int, top_k: int, dev: torch.device, stream: Optional[torch.cuda.Stream]
+             ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    return (_new((n, n_given), torch.float32, dev, stream), _new((n,), torch.float32, dev, stream),
+            _new((n, top_k), torch.int32, dev, stream), _new((n, top_k), torch.float32, dev, stream))
 
 
 def radix_token_logprobs(logits: torch.Tensor, given: Optional[torch.Tensor], ws: torch.Tensor, top_k: int = 0,
@@ -584,7 +592,7 @@ def radix_token_logprobs(logits: torch.Tensor, given: Optional[torch.Tensor], ws
     n, vocab = logits.shape
     g = _given(given, n)
     _same_device(logits.device, given=given, ws=ws, status=status)
-    out = _answers(n, g, max(top_k, 0), logits.device)
+    out = _answers(n, g, max(top_k, 0), logits.device, stream)
     _launch("radix_token_logprobs", logits.device, stream, _ptr(logits), _TORCH_DTYPES[logits.dtype], logits.stride(0) if n > 1 else vocab,
             n, vocab, _ptr(given), g, top_k, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(ws), ws.numel(), _status(status))
     return out
@@ -606,7 +614,7 @@ def radix_score_tokens(model: Model, hidden: torch.Tensor, rows: Optional[torch.
     n = rows.numel() if rows is not None else (n_src if n_rows is None else n_rows)
     g = _given(given, n)
     _same_device(hidden.device, rows=rows, given=given, ws=ws)
-    out = _answers(n, g, max(top_k, 0), hidden.device)
+    out = _answers(n, g, max(top_k, 0), hidden.device, stream)
     _launch("radix_score_tokens", hidden.device, stream, model.handle, _ptr(hidden), n_src, _list(rows, "rows", n), n, _ptr(given), g,
             top_k, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(ws), ws.numel())
     return out

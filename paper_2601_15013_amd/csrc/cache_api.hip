@@ -117,7 +117,7 @@ extern "C" int radix_cache_append(const radix_cache* cache, int32_t layer, const
     const int rc = cache_view(cache, &c);
     if (rc != RADIX_OK) return rc;
     if (layer < 0 || layer >= c.n_layers || B < 0 || N < 0) return RADIX_ERR_BAD_SIZE;
-    if (B > RADIX_CACHE_MAX_LIST) return RADIX_ERR_UNSUPPORTED;
+    if (B > RADIX_CACHE_MAX_LIST || N > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
     if (B == 0 || N == 0) return RADIX_OK;
     if (!k || !v || !cu_seqlens || !past) return RADIX_ERR_NULL_POINTER;
     const int64_t es = cache->dtype == RADIX_F32 ? 4 : 2, row = (int64_t)c.n_kv_heads * c.head_dim;
@@ -145,7 +145,9 @@ extern "C" int radix_paged_attention_workspace_bytes(const radix_cache* cache, i
     PagedShape s;
     rc = paged_shape(c, n_q_heads, max_B, max_N, max_new, &s);
     if (rc != RADIX_OK) return rc;
-    *bytes_out = paged_layout(c, cache->dtype, s).total;
+    const PagedLayout L = paged_layout(c, cache->dtype, s);
+    if (L.items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
+    *bytes_out = L.total;
     return RADIX_OK;
 }
 
@@ -171,7 +173,7 @@ extern "C" int radix_paged_attention(const radix_cache* cache, int32_t layer, co
     s.out_stride = (size_t)out_stride;
     const PagedLayout L = paged_layout(c, cache->dtype, s);
     if (ws_bytes < L.total) return RADIX_ERR_WORKSPACE_TOO_SMALL;
-    if (L.items > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
+    if (L.items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
     launch_paged_plan(c, s, L, cu_seqlens, past, slots, ws, status_dev, (hipStream_t)stream);
     launch_paged_attention(c, cache->dtype, layer, s, L, q, cu_seqlens, past, slots, out, ws, status_dev, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
@@ -180,7 +182,7 @@ extern "C" int radix_paged_attention(const radix_cache* cache, int32_t layer, co
 
 static int check_logprobs(int32_t n_rows, int32_t vocab, int32_t n_given, int32_t top_k) {
     if (n_rows < 0 || vocab <= 0 || n_given < 0 || top_k < 0 || top_k > vocab) return RADIX_ERR_BAD_SIZE;
-    if (top_k > RADIX_MAX_TOP_K) return RADIX_ERR_UNSUPPORTED;
+    if (top_k > RADIX_MAX_TOP_K || n_rows > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
     return RADIX_OK;
 }
 

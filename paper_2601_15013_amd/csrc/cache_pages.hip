@@ -365,7 +365,9 @@ __global__ __launch_bounds__(256) void cache_free_kernel(CacheView c, const int3
     k = k < 0 ? 0 : k;
     const long long from = ((long long)k + c.page_size - 1) / c.page_size;
     for (long long j = from + threadIdx.x; j < c.max_pages; j += 256) {
-        const int page = atomicExch(&c.table[(size_t)s * c.max_pages + j], -1);
+        int32_t* entry = &c.table[(size_t)s * c.max_pages + j];
+        if (*entry == -1) continue;                                         // (most are)
+        const int page = atomicExch(entry, -1);
         if (page == -1) continue;
         if (page < 0 || page >= c.n_pages) { set_status(status, RADIX_ERR_BAD_PAGE); continue; }
         if (atomicSub(&c.refs[page], 1) <= 0) {                             // nobody held it: leave it free

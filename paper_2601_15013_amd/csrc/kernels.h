@@ -216,6 +216,9 @@ static inline AttnPlanLayout attn_plan_layout(size_t N, size_t B) {
 void launch_attn_plan(const int32_t* cu, const int32_t* I_scatter, const int32_t* I_gather, int B, int N,
                       int n_compact, int n_q_heads, int n_kv_heads, int32_t* plan, hipStream_t stream);
 
+// Most workgroups of 256 threads of a launch: a grid has fewer than 2^32 threads.
+constexpr long long MAX_BLOCKS = (1 << 24) - 1;
+
 // ---- paged key/value cache (cache_pages.hip, paged_attention.hip)
 // What the kernels see of a radix_cache.  A piece is one head's keys (or values) of a page; a page of a layer is
 // n_kv_heads pieces of keys, then n_kv_heads pieces of values.
@@ -287,7 +290,7 @@ int launch_paged_attention(const CacheView& c, int dtype, int layer, const Paged
                            hipStream_t stream);
 
 // ---- log-probabilities (token_logprobs.hip): logits [n_rows, vocab] of `dtype`, rows ld elements apart; k <= 32
-size_t token_logprobs_ws_bytes(int n_rows, int k);
+size_t token_logprobs_ws_bytes(int n_rows, int k);       // n_rows <= MAX_BLOCKS
 void launch_token_logprobs(const void* logits, int dtype, size_t ld, int n_rows, int vocab, const int32_t* given, int n_given, int k,
                            float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs, void* ws, int32_t* status,
                            hipStream_t stream);

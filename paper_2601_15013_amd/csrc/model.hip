@@ -638,7 +638,7 @@ int extend_setup(const radix_model* model, const radix_cache* cache, int N, int 
     const size_t hd = c.head_dim, row = (c.n_q_heads + 2 * (size_t)c.n_kv_heads) * hd;
     *s = {c.n_q_heads, B, N, max_new < N ? max_new : N, row, c.n_q_heads * hd};
     *P = paged_layout(*v, cache->dtype, *s);
-    if (P->items > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
+    if (P->items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
     size_t off = align_up(ws_layout(c, model->hilo_layers, (size_t)N, (size_t)B).total, 256);
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes ? bytes : 1, 256); return o; };
     L->past = take((size_t)B * 4);

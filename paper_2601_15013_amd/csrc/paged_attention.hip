@@ -80,7 +80,8 @@ __device__ __forceinline__ int split_length(float work, int target, int least) {
 __device__ __forceinline__ int few_length(float work, const PagedLayout& L) { return split_length(work, L.few_target, 256 / L.few_tile); }
 __device__ __forceinline__ int many_length(float work) { return split_length(work, MANY_TARGET, 1024 / MANY_TILE); }
 __device__ __forceinline__ int splits_of(const PagedCut& k, int few_len, int many_len) {
-    const int length = k.few ? few_len : many_len, n = (int)((unsigned)(k.tiles + (k.few ? length - 1 : 0)) / (unsigned)length);
+    const unsigned length = k.few ? few_len : many_len;
+    const int n = (int)(((unsigned)k.tiles + (k.few ? length - 1 : 0)) / length);
     return n > 1 ? n : 1;
 }
 // Entries of the join for a split sequence: some rows of a kv head each, which all lie in one block.  With few parts eight rows are joined
@@ -499,7 +500,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
     }
     const float sc = 1.4426950408889634f / sqrtf((float)hd);
     // One tile's registers: the next keys are asked for as soon as the scores are formed, the next values as soon as this tile's are
-    // used, so that a tile is on its way nearly all the time; two wavefronts per SIMD keep 128 KB per CU in flight.
+    // used, so that a tile is on its way nearly all the time; three wavefronts per SIMD keep 192 KB per CU in flight.
     typename Tile::K xk;
     typename Tile::V xv;
     typename Tile::Where at = {};
@@ -946,7 +947,7 @@ int launch_paged_attention(const CacheView& c, int dtype, int layer, const Paged
     char* w = (char*)ws;
     PagedArgs a = {c, s, L, cu, past, slots, layer, (int32_t*)ws, (float*)(w + L.few_acc), (float*)(w + L.few_ml),
                    (float*)(w + L.many_acc), (float*)(w + L.many_ml)};
-    if (L.items > 0x7FFFFFFFLL) return RADIX_ERR_UNSUPPORTED;
+    if (L.items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
     const JoinArgs j = {cu, a.plan + L.join, a.plan + L.splits, a.plan + L.slot, a.few_acc, a.few_ml, a.many_acc, a.many_ml, s.B, s.N, s.max_new,
                         c.n_kv_heads, s.n_q_heads / c.n_kv_heads, c.head_dim, L.few_rows, (int)L.few_slots, (int)L.many_slots, (int)s.out_stride,
                         L.many != 0};

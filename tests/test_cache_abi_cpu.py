@@ -112,7 +112,7 @@ def test_append_refuses(lib):
     assert call(ks=511) == BAD_SIZE and call(vs=8) == BAD_SIZE and call(ks=-512) == BAD_SIZE
     assert call(ks=516) == MISALIGNED and call(k=C.c_void_p(0x1008)) == MISALIGNED and call(v=C.c_void_p(0x1002)) == MISALIGNED
     assert call(k=None) == NULL and call(v=None) == NULL and call(cu=None) == NULL and call(past=None) == NULL
-    assert call(B=65536) == UNSUPPORTED
+    assert call(B=65536) == UNSUPPORTED and call(N=1 << 24) == UNSUPPORTED
     assert call(N=0) == 0 and call(B=0) == 0
 
 
@@ -127,6 +127,7 @@ def test_paged_attention_refuses(lib):
     for name in ("q", "cu", "past", "out", "ws"):
         assert call(**{name: None}) == NULL
     assert call(sz=4096) == TOO_SMALL and call(B=65536) == UNSUPPORTED and call(N=1 << 28) == UNSUPPORTED
+    assert call(dtype=0, head_dim=4, qs=32, os_=32, N=1 << 27, new=1 << 27) == UNSUPPORTED                 # 2^26 blocks of 16 rows
     assert call(N=0) == 0 and call(B=0) == 0
 
 
@@ -135,6 +136,7 @@ def test_logprobs_refuse(lib):
         return lib.radix_token_logprobs(x, dt, stride, n, vocab, given, g, k, lp, FAKE, ids, tlp, ws, sz, None, None)
 
     assert call(n=-1) == BAD_SIZE and call(vocab=0) == BAD_SIZE and call(g=-1) == BAD_SIZE and call(k=-1) == BAD_SIZE
+    assert call(n=1 << 24) == UNSUPPORTED
     assert call(vocab=20, k=21) == BAD_SIZE and call(k=33) == UNSUPPORTED and call(dt=5) == UNSUPPORTED and call(stride=99) == BAD_SIZE
     for name in ("x", "given", "lp", "ids", "tlp", "ws"):
         assert call(**{name: None}) == NULL
