@@ -414,7 +414,10 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  *                 multiple of n_kv_heads (query head h reads kv head h / (n_q_heads / n_kv_heads)); alignment as above;
  *                 scores are scaled by 1 / sqrt(head_dim)
  *   max_new       >= tokens of any sequence of the call (host value, sizes the grid)
- *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new), 256-byte aligned
+ *   find_shared   1: sequences that stand next to each other in the batch, have the same number of new tokens (two of them fit 16
+ *                 rows of query heads per kv head) and begin with the same pages, 256 positions or more, attend to those together,
+ *                 so that they are read once for several sequences: forks of one prompt.  Two more launches, about 10 us.  0: not
+ *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new, find_shared), 256-byte aligned
  * past[b] < 0: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position have
  * no influence; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).
  * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values.
@@ -425,16 +428,17 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  * would take 2^24 workgroups.
  */
 int radix_paged_attention_workspace_bytes(const radix_cache* cache, int32_t n_q_heads, int32_t max_N, int32_t max_B,
-                                          int32_t max_new, size_t* bytes_out);
+                                          int32_t max_new, int32_t find_shared, size_t* bytes_out);
 int radix_paged_attention(const radix_cache* cache, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,
                           const int32_t* cu_seqlens, const int32_t* past, const int32_t* slots, int32_t B, int32_t N,
-                          int32_t max_new, void* out, int64_t out_stride, void* ws, size_t ws_bytes, int32_t* status_dev,
-                          void* stream);
+                          int32_t max_new, int32_t find_shared, void* out, int64_t out_stride, void* ws, size_t ws_bytes,
+                          int32_t* status_dev, void* stream);
 
 /*
  * radix_extend_forward - forward of new tokens behind what a cache holds: a chunk of a prompt, the next token of a generation, or
  * both in one batch.  Runs radix_cache_extend for the batch, then the layers over the N new tokens at positions past[b] + offset,
- * storing their keys and values and attending over the cache.
+ * storing their keys and values and attending over the cache (pages that neighbours in the batch share are looked for, once for all
+ * layers).
  *   tok           int32[N], cu_seqlens int32[B+1] (0 .. N), slots int32[B] or NULL, max_new >= new tokens of any sequence
  *   out           float[N, d]: final-RMSNorm hidden states, as from radix_prefill_forward
  *   ws            at least radix_extend_workspace_bytes(model, cache, N, B, max_new), 256-byte aligned

@@ -118,8 +118,8 @@ def _lib() -> C.CDLL:
         lib.radix_cache_compact.argtypes = [cache, vp, vp, sz, vp, vp]
         lib.radix_cache_copy_pages.argtypes = [cache, vp, vp, i32, vp, sz, vp, vp]
         lib.radix_cache_append.argtypes = [cache, i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, vp, vp]
-        lib.radix_paged_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, szp]
-        lib.radix_paged_attention.argtypes = [cache, i32, vp, i64, i32, vp, vp, vp, i32, i32, i32, vp, i64, vp, sz, vp, vp]
+        lib.radix_paged_attention_workspace_bytes.argtypes = [cache, i32, i32, i32, i32, i32, szp]
+        lib.radix_paged_attention.argtypes = [cache, i32, vp, i64, i32, vp, vp, vp, i32, i32, i32, i32, vp, i64, vp, sz, vp, vp]
         lib.radix_extend_workspace_bytes.argtypes = [vp, cache, i32, i32, i32, szp]
         lib.radix_extend_forward.argtypes = [vp, cache, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
         lib.radix_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32, szp]
@@ -519,17 +519,20 @@ def radix_cache_append(cache: Cache, layer: int, k: torch.Tensor, v: torch.Tenso
             _list(past, "past", B), _list(slots, "slots", B), B, N, _status(status))
 
 
-def radix_paged_attention_workspace_bytes(cache: Cache, n_q_heads: int, max_N: int, max_B: int, max_new: int) -> int:
+def radix_paged_attention_workspace_bytes(cache: Cache, n_q_heads: int, max_N: int, max_B: int, max_new: int,
+                                          find_shared: bool = False) -> int:
     n = C.c_size_t()
-    _check(_lib().radix_paged_attention_workspace_bytes(cache.ref, n_q_heads, max_N, max_B, max_new, C.byref(n)),
-           "radix_paged_attention_workspace_bytes")
+    _check(_lib().radix_paged_attention_workspace_bytes(cache.ref, n_q_heads, max_N, max_B, max_new, int(find_shared),
+                                                        C.byref(n)), "radix_paged_attention_workspace_bytes")
     return n.value
 
 
 def radix_paged_attention(cache: Cache, layer: int, q: torch.Tensor, cu_seqlens: torch.Tensor, past: torch.Tensor, max_new: int,
                           ws: torch.Tensor, slots: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                          status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """q: [N, n_q_heads, head_dim], may be a view into fused rows; returns out of that shape."""
+                          status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                          find_shared: bool = False) -> torch.Tensor:
+    """q: [N, n_q_heads, head_dim], may be a view into fused rows; returns out of that shape.  find_shared: see radixmlp.h (pages that
+    neighbours in the batch have in common are read once for several of them)."""
     B, N = _i32(cu_seqlens, "cu_seqlens").numel() - 1, q.shape[0]
     qs = _token_rows(q, "q", cache)
     if out is None:
@@ -539,7 +542,8 @@ def radix_paged_attention(cache: Cache, layer: int, q: torch.Tensor, cu_seqlens:
     os_ = _token_rows(out, "out", cache)
     _same_device(cache.device, q=q, cu_seqlens=cu_seqlens, past=past, ws=ws, slots=slots, out=out, status=status)
     _launch("radix_paged_attention", cache.device, stream, cache.ref, layer, _ptr(q), qs, q.shape[1], _ptr(cu_seqlens),
-            _list(past, "past", B), _list(slots, "slots", B), B, N, max_new, _ptr(out), os_, _ptr(ws), ws.numel(), _status(status))
+            _list(past, "past", B), _list(slots, "slots", B), B, N, max_new, int(find_shared), _ptr(out), os_, _ptr(ws), ws.numel(),
+            _status(status))
     return out
 
 

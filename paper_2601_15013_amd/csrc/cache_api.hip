@@ -129,21 +129,21 @@ extern "C" int radix_cache_append(const radix_cache* cache, int32_t layer, const
     return RADIX_OK;
 }
 
-static int paged_shape(const CacheView& c, int32_t n_q_heads, int32_t B, int32_t N, int32_t max_new, PagedShape* s) {
+static int paged_shape(const CacheView& c, int32_t n_q_heads, int32_t B, int32_t N, int32_t max_new, int32_t find_shared, PagedShape* s) {
     if (B < 0 || N < 0 || max_new < 0 || n_q_heads <= 0 || n_q_heads % c.n_kv_heads != 0) return RADIX_ERR_BAD_SIZE;
     if (B > RADIX_CACHE_MAX_LIST || (int64_t)N * n_q_heads > INT32_MAX || (int64_t)B * n_q_heads > INT32_MAX / 4) return RADIX_ERR_UNSUPPORTED;
-    *s = {n_q_heads, B, N, max_new < N ? max_new : N, 0, 0};
+    *s = {n_q_heads, B, N, max_new < N ? max_new : N, find_shared != 0, 0, 0};
     return RADIX_OK;
 }
 
 extern "C" int radix_paged_attention_workspace_bytes(const radix_cache* cache, int32_t n_q_heads, int32_t max_N, int32_t max_B,
-                                                     int32_t max_new, size_t* bytes_out) {
+                                                     int32_t max_new, int32_t find_shared, size_t* bytes_out) {
     if (!cache || !bytes_out) return RADIX_ERR_NULL_POINTER;
     CacheView c;
     int rc = cache_shape(cache, &c);
     if (rc != RADIX_OK) return rc;
     PagedShape s;
-    rc = paged_shape(c, n_q_heads, max_B, max_N, max_new, &s);
+    rc = paged_shape(c, n_q_heads, max_B, max_N, max_new, find_shared, &s);
     if (rc != RADIX_OK) return rc;
     const PagedLayout L = paged_layout(c, cache->dtype, s);
     if (L.items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
@@ -153,14 +153,14 @@ extern "C" int radix_paged_attention_workspace_bytes(const radix_cache* cache, i
 
 extern "C" int radix_paged_attention(const radix_cache* cache, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,
                                      const int32_t* cu_seqlens, const int32_t* past, const int32_t* slots, int32_t B, int32_t N,
-                                     int32_t max_new, void* out, int64_t out_stride, void* ws, size_t ws_bytes, int32_t* status_dev,
+                                     int32_t max_new, int32_t find_shared, void* out, int64_t out_stride, void* ws, size_t ws_bytes, int32_t* status_dev,
                                      void* stream) {
     CacheView c;
     int rc = cache_view(cache, &c);
     if (rc != RADIX_OK) return rc;
     if (layer < 0 || layer >= c.n_layers) return RADIX_ERR_BAD_SIZE;
     PagedShape s;
-    rc = paged_shape(c, n_q_heads, B, N, max_new, &s);
+    rc = paged_shape(c, n_q_heads, B, N, max_new, find_shared, &s);
     if (rc != RADIX_OK) return rc;
     if (B == 0 || N == 0) return RADIX_OK;
     if (max_new == 0) return RADIX_ERR_BAD_SIZE;

@@ -271,13 +271,14 @@ void launch_cache_append(const CacheView& c, int layer, const void* k, const voi
 // split over several workgroups where the batch has too few blocks for the chip; their results are joined afterwards.
 struct PagedShape {
     int n_q_heads, B, N, max_new;
+    int find_shared;                     // look for sequences that begin with the same pages
     size_t q_stride, out_stride;         // elements between tokens
 };
 // Workspace: prefix sums over the sequences (int32 words; batches too large to be planned by every workgroup) and the partial results.
 struct PagedLayout {
-    size_t item_few, item_many, join, slot, splits;                              // int32 words
+    size_t item_few, item_many, join, slot, splits, common, lead, shared, members;        // int32 words
     size_t few_acc, few_ml, many_acc, many_ml, total;                            // bytes
-    int few_rows, few_tile, few_target, many;        // rows of a block / keys of a tile for few rows; whether there can be blocks of many rows
+    int few_rows, few_tile, few_target, many, share; // rows of a block / keys of a tile for few rows; whether there can be blocks of many rows, or clusters
     long long items, few_slots, many_slots, joins;                           // upper bounds
 };
 PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s);

@@ -636,7 +636,7 @@ int extend_setup(const radix_model* model, const radix_cache* cache, int N, int 
     if (N < 0 || B < 0 || max_new < 0) return RADIX_ERR_BAD_SIZE;
     if (B > RADIX_CACHE_MAX_LIST || (int64_t)N * c.n_q_heads > INT32_MAX || (int64_t)B * c.n_q_heads > INT32_MAX / 4) return RADIX_ERR_UNSUPPORTED;
     const size_t hd = c.head_dim, row = (c.n_q_heads + 2 * (size_t)c.n_kv_heads) * hd;
-    *s = {c.n_q_heads, B, N, max_new < N ? max_new : N, row, c.n_q_heads * hd};
+    *s = {c.n_q_heads, B, N, max_new < N ? max_new : N, 1, row, c.n_q_heads * hd};     // common pages are looked for once, for all layers
     *P = paged_layout(*v, cache->dtype, *s);
     if (P->items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
     size_t off = align_up(ws_layout(c, model->hilo_layers, (size_t)N, (size_t)B).total, 256);

@@ -23,6 +23,7 @@ namespace {
 constexpr int FEW_TARGET = 1536, FEW_TARGET_EVEN = 512, MANY_TARGET = 512;
 constexpr int MANY_ROWS = 128, MANY_TILE = 64;
 constexpr int MAX_HD = 128;
+constexpr long long SHARE_BLOCKS = 8192;                 // most blocks of a batch that is searched for common pages: room for their parts
 
 // Up to PLAN_INLINE sequences every workgroup works out the plan by itself, 64 of them at a time; more are planned by a launch of
 // their own.  A plan launch took 8 us, a third of a short sequence's call.
@@ -94,19 +95,96 @@ __device__ __forceinline__ int join_entries(bool few, int rows, int kv, int spli
     return splits <= 1 ? 0 : (rows + step - 1) / step * kv;
 }
 
+// ------------------------------------------------------------------ sequences that begin with the same pages
+// Forks of one prompt hold the same pages, and decoding them one by one reads those once per sequence while most of a 16-row tile is
+// empty.  So sequences that stand next to each other in the batch and begin with the same pages form a cluster: their rows share tiles
+// over the common keys (all of them before any new token: nothing is masked), then each walks its own keys; the join brings both
+// together.  32 query heads over 8 kv heads, 64 tokens behind 3840 common and 160 own keys: 105 us one by one, 70 with the search for
+// clusters (12 of them its two launches, which a forward makes once for all its layers); 256 tokens of 16 heads behind 2048 and 32:
+// 181 and 83.  Nothing in common: 167 and 180.
+//
+// One wavefront per sequence: full pages that it has in common with the one before it.
+__global__ __launch_bounds__(256) void paged_common_kernel(CacheView c, PagedShape s, PagedLayout L, const int32_t* __restrict__ cu,
+                                                           const int32_t* __restrict__ past, const int32_t* __restrict__ slots,
+                                                           int32_t* __restrict__ plan) {
+    const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (b >= s.B) return;
+    int n = 0;
+    if (b > 0) {
+        const PagedSeq q = paged_seq(c, s, cu, past, slots, b), p = paged_seq(c, s, cu, past, slots, b - 1);
+        if (q.len > 0 && p.len > 0 && q.n == p.n && 2 * q.n * (s.n_q_heads / c.n_kv_heads) <= L.few_rows) {
+            const int32_t *x = c.table + (size_t)q.row * c.max_pages, *y = c.table + (size_t)p.row * c.max_pages;
+            const int limit = min(q.len, p.len) - q.n, pages = limit >> c.page_shift;
+            for (n = 0; n < pages; n += 64) {
+                const unsigned long long differ = __ballot(n + lane < pages && x[n + lane] != y[n + lane]);
+                if (differ) { n += __ffsll((long long)differ) - 1; break; }
+            }
+            n = min(n, pages);
+        }
+    }
+    if (lane == 0) plan[L.common + b] = n;
+}
+
+// Largest v of this and the threads before it, or `carry`; all threads of the workgroup call.
+__device__ __forceinline__ int block_max(int v, int carry, int* part /* [PT / 64] in LDS */) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(v, o, 64);
+        if (lane >= o) v = max(v, u);
+    }
+    __syncthreads();
+    if (lane == 63) part[wave] = v;
+    __syncthreads();
+    v = max(v, carry);
+    for (int w = 0; w < wave; ++w) v = max(v, part[w]);
+    return v;
+}
+
 // ------------------------------------------------------------------ the plan as a launch of its own (one workgroup)
+// Entry 2 b of the list of items is what the cluster that sequence b leads has in common, entry 2 b + 1 the sequence's own keys.
 __global__ __launch_bounds__(PT) void paged_plan_kernel(CacheView c, PagedShape s, PagedLayout L, const int32_t* __restrict__ cu,
                                                         const int32_t* __restrict__ past, const int32_t* __restrict__ slots,
                                                         int32_t* __restrict__ plan, int32_t* status) {
     __shared__ long long part[PT / 64];
     __shared__ float work[2][PT / 64];
+    __shared__ int top[PT / 64];
+    __shared__ int carry;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, group = s.n_q_heads / c.n_kv_heads;
+    int32_t *common = plan + L.common, *lead = plan + L.lead, *shared = plan + L.shared, *members = plan + L.members;
+    // clusters: runs of sequences that have enough in common with the one before, cut where 16 rows are full
+    const int tile_shift = L.few_tile == 16 ? 4 : 5, enough = 256;
+    auto goes_on = [&](int b) { return b > 0 && b < s.B && (long long)common[b] << c.page_shift >= enough; };
+    if (tid == 0) carry = 0;
+    for (int b0 = 0; b0 < s.B; b0 += PT) {
+        const int b = b0 + tid;
+        __syncthreads();
+        const int begin = block_max(L.share && b < s.B && !goes_on(b) ? b : 0, carry, top);         // first sequence of the run
+        __syncthreads();
+        if (tid == PT - 1) carry = begin;
+        if (b < s.B) {
+            lead[b] = -1;
+            shared[b] = members[b] = 0;
+            if (L.share) {
+                const int rows = (cu[b + 1] - cu[b]) * group, fit = rows > 0 && 2 * rows <= L.few_rows ? L.few_rows / rows : 1;
+                const int at = (b - begin) % fit, first = b - at;
+                int n = 1, pages = 0x7FFFFFFF;
+                while (n < fit && goes_on(first + n)) { pages = min(pages, common[first + n]); ++n; }
+                if (n > 1) {
+                    lead[b] = first;
+                    shared[b] = (pages << c.page_shift) >> tile_shift;              // whole tiles
+                    if (at == 0) members[b] = n;
+                }
+            }
+        }
+    }
+    __syncthreads();
     float few_work = 0.f, many_work = 0.f;
     for (int b = tid; b < s.B; b += PT) {
         const PagedSeq q = paged_seq(c, s, cu, past, slots, b);
         const PagedCut k = paged_cut(c, s, L, q);
         if (q.err) set_status(status, q.err);
-        const float w = (float)k.blocks * (float)k.tiles * (float)c.n_kv_heads;
+        const float w = ((float)k.blocks * (float)(k.tiles - shared[b]) + (members[b] ? (float)shared[b] : 0.f)) * (float)c.n_kv_heads;
         few_work += k.few ? w : 0.f;
         many_work += k.few ? 0.f : w;
     }
@@ -121,30 +199,37 @@ __global__ __launch_bounds__(PT) void paged_plan_kernel(CacheView c, PagedShape 
     for (int b0 = 0; b0 < s.B; b0 += PT) {
         const int b = b0 + tid;
         PagedCut k = {true, 0, 0};
-        int splits = 1, rows = 0;
+        int rows = 0, splits = 1, splits_shared = 0, parts = 0;         // parts: of a row of the sequence, the common ones included
         if (b < s.B) {
             const PagedSeq q = paged_seq(c, s, cu, past, slots, b);
             k = paged_cut(c, s, L, q);
-            splits = splits_of(k, few_len, many_len);
+            k.tiles -= shared[b];
+            splits = parts = splits_of(k, few_len, many_len);
+            if (lead[b] >= 0) parts += splits_of({true, 1, shared[b]}, few_len, many_len);
+            if (members[b]) splits_shared = parts - splits;
             rows = q.n * group;
         }
-        const long long items = (long long)k.blocks * c.n_kv_heads * splits;
+        const long long items = (long long)k.blocks * c.n_kv_heads * splits, items_shared = (long long)splits_shared * c.n_kv_heads;
         const int sh = k.few ? 0 : 32;
         long long ti, ts, tr;
-        const long long i0 = run_items + block_exclusive(items << sh, &ti, part);
-        const long long s0 = run_slots + block_exclusive((splits > 1 ? items : 0) << sh, &ts, part);
-        const long long r0 = run_rows + block_exclusive(join_entries(k.few, rows, c.n_kv_heads, splits), &tr, part);
+        const long long i0 = run_items + block_exclusive((items << sh) + items_shared, &ti, part);
+        const long long s0 = run_slots + block_exclusive(((parts > 1 ? items : 0) << sh) + items_shared, &ts, part);
+        const long long r0 = run_rows + block_exclusive(join_entries(k.few, rows, c.n_kv_heads, parts), &tr, part);
         if (b < s.B) {
-            plan[L.item_few + b] = (int)(i0 & 0xffffffffLL);
+            const int few_at = (int)(i0 & 0xffffffffLL), slot_at = (int)(k.few ? s0 & 0xffffffffLL : s0 >> 32);
+            plan[L.item_few + 2 * b] = few_at;
+            plan[L.item_few + 2 * b + 1] = few_at + (int)items_shared;
             plan[L.item_many + b] = (int)(i0 >> 32);
-            plan[L.slot + b] = (int)(k.few ? s0 & 0xffffffffLL : s0 >> 32);
+            plan[L.slot + 2 * b] = slot_at;
+            plan[L.slot + 2 * b + 1] = slot_at + (k.few ? (int)items_shared : 0);
+            plan[L.splits + 2 * b] = splits_shared;
+            plan[L.splits + 2 * b + 1] = splits;
             plan[L.join + b] = (int)r0;
-            plan[L.splits + b] = splits;
         }
         run_items += ti; run_slots += ts; run_rows += tr;
     }
     if (tid == 0) {
-        plan[L.item_few + s.B] = (int)(run_items & 0xffffffffLL);
+        plan[L.item_few + 2 * s.B] = (int)(run_items & 0xffffffffLL);
         plan[L.item_many + s.B] = (int)(run_items >> 32);
         plan[L.join + s.B] = (int)run_rows;
     }
@@ -152,22 +237,42 @@ __global__ __launch_bounds__(PT) void paged_plan_kernel(CacheView c, PagedShape 
 
 // One entry of the batch's list of items (those of many rows first): its sequence, the entry's number within the sequence, the
 // sequence's splits and where its partial results begin.  By a wavefront.
-struct PagedFound { PagedSeq q; bool few; int in, blocks, splits, slot; };
+// first: first tile.  common: keys that a cluster shares; its members' rows then stand one after the other as those of one sequence would.
+struct PagedFound { PagedSeq q; bool few, common, apart; int in, blocks, splits, slot, first; };       // apart: its results are parts
 // From the lists in the workspace.
 __device__ __forceinline__ bool paged_listed(const PagedArgs& a, int index, int lane, PagedFound& f) {
     const int32_t* many = a.plan + a.L.item_many;
     const int n_many = many[a.s.B];
-    const int32_t* first = index < n_many ? many : a.plan + a.L.item_few;
-    if (index >= n_many) index -= n_many;
-    if (index >= first[a.s.B]) return false;
-    const int b = __builtin_amdgcn_readfirstlane(sequence_of(first, a.s.B, index, lane));
-    f.in = index - first[b];
-    f.splits = a.plan[a.L.splits + b];
-    f.slot = a.plan[a.L.slot + b];
+    int b, e;
+    if (index < n_many) {
+        b = __builtin_amdgcn_readfirstlane(sequence_of(many, a.s.B, index, lane));
+        e = 2 * b + 1;
+        f.in = index - many[b];
+    } else {
+        const int32_t* few = a.plan + a.L.item_few;
+        index -= n_many;
+        if (index >= few[2 * a.s.B]) return false;
+        e = __builtin_amdgcn_readfirstlane(sequence_of(few, 2 * a.s.B, index, lane));
+        b = e >> 1;
+        f.in = index - few[e];
+    }
+    f.common = (e & 1) == 0;
+    f.splits = a.plan[a.L.splits + e];
+    f.slot = a.plan[a.L.slot + e];
     f.q = paged_seq(a.c, a.s, a.cu, a.past, a.slots, b);
     const PagedCut k = paged_cut(a.c, a.s, a.L, f.q);
     f.few = k.few;
     f.blocks = k.blocks;
+    const int shared = a.plan[a.L.shared + b];
+    f.first = f.common ? 0 : shared;
+    f.apart = f.splits > 1 || shared > 0;
+    if (f.common) {
+        const int n = f.q.n * a.plan[a.L.members + b];
+        f.blocks = 1;
+        f.q.len = shared * a.L.few_tile;
+        f.q.n = n <= a.s.N - f.q.from ? n : 0;
+        if (n * (a.s.n_q_heads / a.c.n_kv_heads) > a.L.few_rows || f.q.n == 0 || f.splits < 1) return false;
+    }
     return true;
 }
 // Worked out on the spot, 64 sequences at a time; the first 64, which are often all, stay in registers between the passes.  Workgroup 0
@@ -212,6 +317,8 @@ __device__ __forceinline__ bool paged_planned(const PagedArgs& a, int index, int
     }
     int at = 0, at_few = 0, at_many = 0, at_join = 0;
     bool found = false;
+    f.common = false;
+    f.first = 0;
 #pragma unroll 1
     for (int b0 = 0; b0 <= last; b0 += 64) {
         if (b0 > 0) fetch(b0 + lane);
@@ -223,12 +330,13 @@ __device__ __forceinline__ bool paged_planned(const PagedArgs& a, int index, int
         int many_parts = at_many;
         if (a.L.many) many_parts += wave_inclusive(k.few ? 0 : parts);
         const int slot = (k.few ? few_parts : many_parts) - parts;
-        if (writer) {
+        if (writer) {                                       // (in the form of the plan's own launch: no sequence leads a cluster)
             const int joins = join_entries(k.few, q.n * group, kv, splits), join_incl = wave_inclusive(joins) + at_join;
             if (b0 + lane < a.s.B) {
                 plan[a.L.join + b0 + lane + 1] = join_incl;
-                plan[a.L.slot + b0 + lane] = slot;
-                plan[a.L.splits + b0 + lane] = splits;
+                plan[a.L.slot + 2 * (b0 + lane) + 1] = slot;
+                plan[a.L.splits + 2 * (b0 + lane) + 1] = splits;
+                plan[a.L.lead + b0 + lane] = -1;
                 if (b0 + lane == 0) plan[a.L.join] = 0;
             }
             at_join = __builtin_amdgcn_readlane(join_incl, 63);
@@ -241,6 +349,7 @@ __device__ __forceinline__ bool paged_planned(const PagedArgs& a, int index, int
             f.in = index - __builtin_amdgcn_readlane(incl - mine, l);
             f.blocks = __builtin_amdgcn_readlane(k.blocks, l);
             f.splits = __builtin_amdgcn_readlane(splits, l);
+            f.apart = f.splits > 1;
             f.slot = __builtin_amdgcn_readlane(slot, l);
             f.q.from = __builtin_amdgcn_readlane(q.from, l);
             f.q.n = __builtin_amdgcn_readlane(q.n, l);
@@ -256,16 +365,16 @@ __device__ __forceinline__ bool paged_planned(const PagedArgs& a, int index, int
 }
 // (sums over a malformed cu_seqlens may have wrapped: nothing leaves the lists' room)
 __device__ __forceinline__ bool paged_find(const PagedArgs& a, int lane, PagedFound& f, int32_t* status) {
-    const bool found = a.s.B > PLAN_INLINE ? paged_listed(a, blockIdx.x, lane, f) : paged_planned(a, blockIdx.x, lane, f, a.plan, status);
+    const bool found = a.s.B > PLAN_INLINE || a.L.share ? paged_listed(a, blockIdx.x, lane, f) : paged_planned(a, blockIdx.x, lane, f, a.plan, status);
     if (!found) return false;
     const long long items = (long long)f.blocks * a.c.n_kv_heads * f.splits;
-    return f.in >= 0 && f.in < items && (f.splits == 1 || (f.slot >= 0 && f.slot + items <= (f.few ? a.L.few_slots : a.L.many_slots)));
+    return f.in >= 0 && f.in < items && (!f.apart || (f.slot >= 0 && f.slot + items <= (f.few ? a.L.few_slots : a.L.many_slots)));
 }
 
 // A work item: the kv head, block and split of a sequence; `slot` of its partial result where the block is split.
 // Items of a sequence: kv heads fastest, so that consecutive workgroups - and with them the eight XCDs - take different heads, and
 // the blocks of one head, which read the same keys, meet in one L2; then the splits; then the blocks, the last (longest) first.
-struct PagedItem { PagedSeq q; int kvh, blk, split, splits, slot; };
+struct PagedItem { PagedSeq q; int kvh, blk, split, splits, slot, first; bool common, apart; };
 __device__ __forceinline__ PagedItem paged_item(const PagedArgs& a, const PagedFound& f) {
     auto u = [](int x) { return __builtin_amdgcn_readfirstlane(x); };        // the same in all lanes, which not every path tells
     const int kv = a.c.n_kv_heads, in = u(f.in), splits = u(f.splits), rest = in / kv;
@@ -276,6 +385,9 @@ __device__ __forceinline__ PagedItem paged_item(const PagedArgs& a, const PagedF
     w.split = rest % splits;
     w.blk = u(f.blocks) - 1 - rest / splits;
     w.slot = u(f.slot) + in;
+    w.first = u(f.first);
+    w.common = u((int)f.common) != 0;
+    w.apart = u((int)f.apart) != 0;
     return w;
 }
 
@@ -477,8 +589,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
     const int row0 = w.blk * ROWS, last = sq.len - 1;
     // the item's tiles: its share of those up to the last position that a row of the block sees
     const int last_row = min(row0 + ROWS, rows) - 1;
-    const int tiles = sq.len > 0 ? (past + last_row / group) / Tile::KEYS + 1 : 0;
-    const int t0 = part_begin(tiles, w.split, w.splits), t1 = part_begin(tiles, w.split + 1, w.splits);
+    const int tiles = w.common ? sq.len / Tile::KEYS : sq.len > 0 ? (past + last_row / group) / Tile::KEYS + 1 : 0;
+    const int t0 = w.first + part_begin(tiles - w.first, w.split, w.splits), t1 = w.first + part_begin(tiles - w.first, w.split + 1, w.splits);
     const int32_t* table = a.c.table + (size_t)sq.row * a.c.max_pages;
     const char* base = a.c.pages + (size_t)a.layer * a.c.layer_bytes + (size_t)w.kvh * a.c.piece_bytes;
 
@@ -487,7 +599,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int row = row0 + 16 * nt + r, j = min(row, last_row) / group, h = w.kvh * group + min(row, last_row) % group;
-        limit[nt] = past + j;
+        limit[nt] = w.common ? last : past + j;
         tile.load_q(q + (size_t)(sq.from + j) * a.s.q_stride + (size_t)h * hd, nt, row <= last_row, hd, lane);
     }
     f32x4 acc[NT][NA];
@@ -582,7 +694,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
 #pragma unroll
             for (int u = 0; u < 4; ++u) o[u] = fmaf(f, so[k][row][e + u], o[u]);
         }
-        if (w.splits > 1) {
+        if (w.apart) {
             const size_t at = (size_t)w.slot * ROWS + row;
             *reinterpret_cast<f32x4*>(a.few_acc + at * MAX_HD + e) = f32x4{o[0], o[1], o[2], o[3]};
             if (e == 0) { a.few_ml[2 * at] = top; a.few_ml[2 * at + 1] = sum; }
@@ -812,8 +924,9 @@ __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedArgs a, const 
 // Joins the parts of split blocks; workgroups take entries in turn.  Groups of 32 lanes, four elements a lane: with few parts a group joins a row by itself, with more
 // the eight groups take every eighth part of one row and their sums are added in order.
 struct JoinArgs {
-    const int32_t *cu, *first, *splits, *slot;
-    const float *few_acc, *few_ml, *many_acc, *many_ml;
+    const int32_t *cu, *first, *splits, *slot, *lead;
+    const char* ws;
+    uint32_t few_acc, few_ml, many_acc, many_ml;             // bytes from ws
     int B, N, max_new, kv, group, hd, few_rows, few_slots, many_slots, out_stride;
     bool many;
 };
@@ -828,22 +941,28 @@ __global__ __launch_bounds__(256) void paged_join_kernel(JoinArgs a, T* __restri
         int kv = a.kv, group = a.group;
         asm volatile("" : "+s"(kv), "+s"(group));          // what their divisions need is made anew: held over the loop it would not fit
         const int b = __builtin_amdgcn_readfirstlane(sequence_of(a.first, a.B, index, lane));
-        const int in = index - a.first[b], splits = a.splits[b], slot = a.slot[b], from = a.cu[b], n = a.cu[b + 1] - from, rows = n * group;
+        const int in = index - a.first[b], own = a.splits[2 * b + 1], slot = a.slot[2 * b + 1], from = a.cu[b], n = a.cu[b + 1] - from;
         if (from < 0 || n <= 0 || n > a.max_new || from > a.N - n) continue;
+        const int rows = n * group, lead = a.lead[b], before = lead >= 0 ? a.splits[2 * lead] : 0, splits = before + own;
         const bool few = !a.many || rows <= a.few_rows, together = splits > JOIN_ALONE;
         const int block = few ? a.few_rows : MANY_ROWS, blocks = (rows + block - 1) / block;
         const int step = join_step(splits), count = join_rows(few, splits);
-        const int kvh = in % kv, row0 = in / kv * count, end = min(row0 + count, rows);
-        if (in < 0 || row0 >= rows || slot < 0 || slot + (long long)blocks * kv * splits > (few ? a.few_slots : a.many_slots)) continue;
-        const float* acc = few ? a.few_acc : a.many_acc;
-        const float* ml = few ? a.few_ml : a.many_ml;
-        int slot0 = slot + (blocks - 1 - row0 / block) * splits * kv + kvh;               // 32 bits hold any place in the parts' room
-        asm volatile("" : "+v"(slot0));                    // (addresses in vector registers: there are plenty)
+        const int kvh = in % kv, row0 = in / kv * count, end = min(row0 + count, rows), room = few ? a.few_slots : a.many_slots;
+        if (in < 0 || row0 >= rows || slot < 0 || slot + (long long)blocks * kv * own > room) continue;
+        // parts 0 .. before - 1: those of the cluster, where the sequence's rows begin at row (b - lead) * rows
+        const int lead_slot = lead >= 0 ? a.slot[2 * lead] : 0, lead_row = lead >= 0 ? (b - lead) * rows : 0;
+        if (lead_slot < 0 || lead_slot + (long long)kv * before > room || lead_row < 0 || lead_row + rows > (lead >= 0 ? block : rows)) continue;
+        const float* acc = reinterpret_cast<const float*>(a.ws + (few ? a.few_acc : a.many_acc));
+        const float* ml = reinterpret_cast<const float*>(a.ws + (few ? a.few_ml : a.many_ml));
+        // 32 bits hold any place in the parts' room; places in vector registers: there are plenty
+        int own_at = (slot + (blocks - 1 - row0 / block) * own * kv + kvh) * block, lead_at = (lead_slot + kvh) * block + lead_row;
+        int before_v = before, stride_v = kv * block;
+        asm volatile("" : "+v"(own_at), "+v"(lead_at), "+v"(before_v), "+v"(stride_v));
 #pragma unroll 1
         for (int r0 = row0; r0 < end; r0 += step) {
             const int row = together ? r0 : r0 + part;
             const bool active = row < end;
-            auto at = [&](int k) { return (slot0 + k * kv) * block + (row & (block - 1)); };
+            auto at = [&](int k) { return (k < before_v ? lead_at + k * stride_v : own_at + (k - before_v) * stride_v) + (row & (block - 1)); };
             float top = -INFINITY, sum = 0.f;
             f32x4 o = {0.f, 0.f, 0.f, 0.f};
             auto add = [&](int k, float use) {
@@ -907,23 +1026,30 @@ PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s) {
     const long long N = s.N, B = s.B, kv = c.n_kv_heads;
     // blocks of sequence b: at most rows / block + 1, and none without tokens
     const long long few_blocks = dtype == RADIX_F32 ? N * group / 16 + B : (B < N ? B : N), many_blocks = L.many ? N * group / MANY_ROWS + B : 0;
-    L.items = few_blocks * kv + FEW_TARGET + (L.many ? many_blocks * kv + MANY_TARGET : 0);
     // (ceil(x) < 2 x where it is more than one)
     // With few blocks all parts are of about one length, and two workgroups a CU that are done together beat any more; many blocks of
     // different lengths even out in more parts.  One token behind 131071 keys, 8 kv heads: 88.9 us in 512 parts, 92.9 in 768, 94 in 1024
     // and more; 64 tokens behind 500 to 4000 keys: 121 us for 512, 111 for 1024, 106.6 for 1536, 107.8 for 2048.
     L.few_target = few_blocks * kv < FEW_TARGET_EVEN / 2 ? FEW_TARGET_EVEN : FEW_TARGET;
-    L.few_slots = 2 * FEW_TARGET;
+    // clusters (two sequences at the least have to fit a block): what of them is not split is a part all the same
+    const long long shared_blocks = B * kv < SHARE_BLOCKS ? B * kv : SHARE_BLOCKS;
+    L.share = s.find_shared && B > 1 && B * kv <= SHARE_BLOCKS && 2 * group <= L.few_rows;
+    L.few_slots = 2 * FEW_TARGET + (s.find_shared ? 2 * shared_blocks : 0);
     L.many_slots = L.many ? MANY_TARGET : 0;
+    L.items = few_blocks * kv * (L.share ? 2 : 1) + FEW_TARGET + (L.many ? many_blocks * kv + MANY_TARGET : 0);
     // entries of the join: a row at the least; none where a row of the table holds no more than one part (few_length, many_length)
     L.joins = (long long)c.max_pages * c.page_size <= 256 ? 0 : N * s.n_q_heads;
     size_t w = 64;
     auto words = [&](size_t n) { const size_t o = w; w += n; return o; };
-    L.item_few = words((size_t)B + 1);
+    L.item_few = words(2 * (size_t)B + 1);
     L.item_many = words((size_t)B + 1);
     L.join = words((size_t)B + 1);
-    L.slot = words((size_t)B);
-    L.splits = words((size_t)B);
+    L.slot = words(2 * (size_t)B);
+    L.splits = words(2 * (size_t)B);
+    L.common = words((size_t)B);
+    L.lead = words((size_t)B);
+    L.shared = words((size_t)B);
+    L.members = words((size_t)B);
     size_t off = align_up(w * 4, 256);
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
     // up to 16 rows a block, or 32: room for either, so that the size grows with max_new
@@ -937,7 +1063,9 @@ PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s) {
 
 void launch_paged_plan(const CacheView& c, const PagedShape& s, const PagedLayout& L, const int32_t* cu, const int32_t* past,
                        const int32_t* slots, void* ws, int32_t* status, hipStream_t stream) {
-    if (s.B > PLAN_INLINE)
+    if (L.share)
+        hipLaunchKernelGGL(paged_common_kernel, dim3((unsigned)ceil_div(s.B, 4)), dim3(256), 0, stream, c, s, L, cu, past, slots, (int32_t*)ws);
+    if (L.share || s.B > PLAN_INLINE)
         hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(PT), 0, stream, c, s, L, cu, past, slots, (int32_t*)ws, status);
 }
 
@@ -948,7 +1076,8 @@ int launch_paged_attention(const CacheView& c, int dtype, int layer, const Paged
     PagedArgs a = {c, s, L, cu, past, slots, layer, (int32_t*)ws, (float*)(w + L.few_acc), (float*)(w + L.few_ml),
                    (float*)(w + L.many_acc), (float*)(w + L.many_ml)};
     if (L.items > MAX_BLOCKS) return RADIX_ERR_UNSUPPORTED;
-    const JoinArgs j = {cu, a.plan + L.join, a.plan + L.splits, a.plan + L.slot, a.few_acc, a.few_ml, a.many_acc, a.many_ml, s.B, s.N, s.max_new,
+    const JoinArgs j = {cu, a.plan + L.join, a.plan + L.splits, a.plan + L.slot, a.plan + L.lead, w, (uint32_t)L.few_acc, (uint32_t)L.few_ml,
+                        (uint32_t)L.many_acc, (uint32_t)L.many_ml, s.B, s.N, s.max_new,
                         c.n_kv_heads, s.n_q_heads / c.n_kv_heads, c.head_dim, L.few_rows, (int)L.few_slots, (int)L.many_slots, (int)s.out_stride,
                         L.many != 0};
     const dim3 grid((unsigned)L.items), block(256), join((unsigned)(L.joins > 1024 ? 1024 : L.joins));

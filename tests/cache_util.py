@@ -119,13 +119,12 @@ def random_cache(seed, lens, kv, hd, page, dtype, layers=1, spare=3, extra_pages
     return binding.Cache(pages.cuda(), i32(refs), i32(table), i32(list(lens)))
 
 
-def rows_of(cache, layer, slot, n, kind):
+def rows_of(cache, layer, slot, n, kind, pages=None, table=None):
     """Keys (0) or values (1) of positions 0 .. n - 1 of a slot in 64 bits: [n, kv, hd] on the CPU."""
-    page = cache.pages.shape[4]
-    table = cache.page_table[slot].tolist()
-    pages = cache.pages[layer, :, kind].cpu().double()
-    out = [pages[table[p // page], :, p % page] for p in range(n)]
-    return torch.stack(out) if out else torch.zeros((0,) + tuple(pages.shape[1:2]) + (pages.shape[3],), dtype=torch.float64)
+    pages = cache.pages[layer].cpu() if pages is None else pages
+    table = cache.page_table.cpu().long() if table is None else table
+    at, page = torch.arange(n), pages.shape[3]
+    return pages[table[slot, at // page], kind, :, at % page].double()
 
 
 def attention_ref(cache, layer, q, cu, past, slots=None):
@@ -133,12 +132,12 @@ def attention_ref(cache, layer, q, cu, past, slots=None):
     q = q.cpu().double()
     N, hq, hd = q.shape
     o, a = torch.zeros_like(q), torch.zeros_like(q)
+    pages, table = cache.pages[layer].cpu(), cache.page_table.cpu().long()
     for b in range(len(cu) - 1):
         n = cu[b + 1] - cu[b]
         if n <= 0 or past[b] < 0:
             continue
-        k = rows_of(cache, layer, slots[b] if slots else b, past[b] + n, 0)
-        v = rows_of(cache, layer, slots[b] if slots else b, past[b] + n, 1)
+        k, v = (rows_of(cache, layer, slots[b] if slots else b, past[b] + n, kind, pages, table) for kind in (0, 1))
         g = hq // k.shape[1]
         for h in range(hq):
             s = q[cu[b]:cu[b + 1], h] @ k[:, h // g].T / hd ** 0.5

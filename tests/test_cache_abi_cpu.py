@@ -40,7 +40,7 @@ def test_shapes_of_a_cache(lib, kw, code):
     assert lib.radix_cache_workspace_bytes(cache(**kw), 4, C.byref(n)) == code
     assert lib.radix_cache_reset(cache(**kw), None) == code
     assert lib.radix_cache_append(cache(**kw), 0, FAKE, 512, FAKE, 512, FAKE, FAKE, None, 1, 1, None, None) == code
-    assert lib.radix_paged_attention_workspace_bytes(cache(**kw), 8, 4, 1, 4, C.byref(n)) == code
+    assert lib.radix_paged_attention_workspace_bytes(cache(**kw), 8, 4, 1, 4, 0, C.byref(n)) == code
 
 
 @pytest.mark.parametrize("field", ["pages", "page_refs", "page_table", "seq_lens"])
@@ -49,7 +49,7 @@ def test_missing_arrays(lib, field):
     assert lib.radix_cache_reset(c, None) == NULL
     assert lib.radix_cache_extend(c, None, FAKE, 1, FAKE, FAKE, BIG, None, None) == NULL
     assert lib.radix_cache_free(c, FAKE, None, 1, None, None) == NULL
-    assert lib.radix_paged_attention(c, 0, FAKE, 1024, 8, FAKE, FAKE, None, 1, 1, 1, FAKE, 1024, FAKE, BIG, None, None) == NULL
+    assert lib.radix_paged_attention(c, 0, FAKE, 1024, 8, FAKE, FAKE, None, 1, 1, 1, 0, FAKE, 1024, FAKE, BIG, None, None) == NULL
 
 
 def test_sizes(lib):
@@ -67,22 +67,23 @@ def test_sizes(lib):
     assert lib.radix_cache_workspace_bytes(cache(), 65536, C.byref(n)) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("share", [0, 1])
 @pytest.mark.parametrize("dtype", [0, 1, 2])
-def test_the_attention_workspace_grows_with_its_bounds(lib, dtype):
+def test_the_attention_workspace_grows_with_its_bounds(lib, dtype, share):
     n = C.c_size_t()
 
     def size(N, B, new):
-        assert lib.radix_paged_attention_workspace_bytes(cache(dtype=dtype), 8, N, B, new, C.byref(n)) == 0
+        assert lib.radix_paged_attention_workspace_bytes(cache(dtype=dtype), 8, N, B, new, share, C.byref(n)) == 0
         return n.value
 
-    for grow in ([(1, 1, 1), (8, 8, 1), (100, 100, 1), (4000, 4000, 1)], [(200, 10, 1), (200, 10, 8), (200, 10, 17), (200, 10, 100), (200, 10, 200)],
+    for grow in ([(1, 1, 1), (8, 8, 1), (100, 100, 1), (2000, 2000, 1), (2100, 2100, 1), (4000, 4000, 1)], [(200, 10, 1), (200, 10, 8), (200, 10, 17), (200, 10, 100), (200, 10, 200)],
                  [(100, 1, 100), (1000, 1, 100), (1000, 1, 1000), (1000, 9, 1000)]):
         sizes = [size(*g) for g in grow]
         assert sizes == sorted(sizes)
-    assert lib.radix_paged_attention_workspace_bytes(cache(), 6, 4, 1, 4, C.byref(n)) == BAD_SIZE         # 4 kv heads do not divide 6
-    assert lib.radix_paged_attention_workspace_bytes(cache(), 8, 1 << 29, 1, 4, C.byref(n)) == UNSUPPORTED
-    assert lib.radix_paged_attention_workspace_bytes(cache(), 8, -1, 1, 4, C.byref(n)) == BAD_SIZE
-    assert lib.radix_paged_attention_workspace_bytes(None, 8, 1, 1, 4, C.byref(n)) == NULL
+    assert lib.radix_paged_attention_workspace_bytes(cache(), 6, 4, 1, 4, 0, C.byref(n)) == BAD_SIZE         # 4 kv heads do not divide 6
+    assert lib.radix_paged_attention_workspace_bytes(cache(), 8, 1 << 29, 1, 4, 0, C.byref(n)) == UNSUPPORTED
+    assert lib.radix_paged_attention_workspace_bytes(cache(), 8, -1, 1, 4, 0, C.byref(n)) == BAD_SIZE
+    assert lib.radix_paged_attention_workspace_bytes(None, 8, 1, 1, 4, 0, C.byref(n)) == NULL
 
 
 def test_page_calls_refuse(lib):
@@ -118,7 +119,7 @@ def test_append_refuses(lib):
 
 def test_paged_attention_refuses(lib):
     def call(layer=0, q=FAKE, qs=1024, hq=8, cu=FAKE, past=FAKE, B=1, N=4, new=4, out=FAKE, os_=1024, ws=FAKE, sz=BIG, **kw):
-        return lib.radix_paged_attention(cache(**kw), layer, q, qs, hq, cu, past, None, B, N, new, out, os_, ws, sz, None, None)
+        return lib.radix_paged_attention(cache(**kw), layer, q, qs, hq, cu, past, None, B, N, new, 1, out, os_, ws, sz, None, None)
 
     assert call(layer=2) == BAD_SIZE and call(layer=-1) == BAD_SIZE and call(hq=6) == BAD_SIZE and call(hq=0) == BAD_SIZE
     assert call(B=-1) == BAD_SIZE and call(N=-1) == BAD_SIZE and call(new=-1) == BAD_SIZE and call(new=0) == BAD_SIZE

@@ -12,12 +12,12 @@ pytestmark = pytest.mark.gpu
 BAD_CU, BAD_PAGE, BAD_SLOT = -6, -11, -13
 
 
-def attend(cache, q, cu, past, max_new, slots=None, layer=0, status=None, out=None, stream=None):
+def attend(cache, q, cu, past, max_new, slots=None, layer=0, status=None, out=None, stream=None, share=False):
     B = len(cu) - 1
-    ws = binding.alloc_workspace(binding.radix_paged_attention_workspace_bytes(cache, q.shape[1], q.shape[0], B, max_new))
+    ws = binding.alloc_workspace(binding.radix_paged_attention_workspace_bytes(cache, q.shape[1], q.shape[0], B, max_new, share))
     ws.fill_(0xFF)                                          # NaN and -1 everywhere: nothing of it may be relied on
     return binding.radix_paged_attention(cache, layer, q, CU.i32(cu), CU.i32(past), max_new, ws, slots=None if slots is None else CU.i32(slots),
-                                         status=status, out=out, stream=stream)
+                                         status=status, out=out, stream=stream, find_shared=share)
 
 
 def queries(seed, N, hq, hd, dtype, fused_with=0):
@@ -187,6 +187,102 @@ def test_numbers_of_sequences_around_the_plan(B, dtype, most):
     past[-1], news[-1] = 1500, 1
     past[B // 2], news[B // 2] = 2500, most
     check(past, news, 4, 2, 128 if dtype != "f32" else 32, 32, dtype)
+
+
+def forks(seed, past, news, groups, kv, hd, page, dtype):
+    """A cache in which the sequences of every (first, count, pages) group begin with the first one's pages."""
+    cache = CU.random_cache(seed, [p + n for p, n in zip(past, news)], kv, hd, page, dtype, poison=True)
+    for first, count, pages in groups:
+        cache.page_table[first + 1:first + count, :pages] = cache.page_table[first, :pages]
+    return cache
+
+
+def check_forks(past, news, groups, hq, kv, hd, page, dtype, slots=None, max_new=None):
+    cache = forks(3, past, news, groups, kv, hd, page, dtype)
+    cu = CU.ragged(news)
+    q = queries(4, cu[-1], hq, hd, dtype)
+    status = CU.status_word()
+    o = attend(cache, q, cu, past, max_new or max(news), status=status, share=True).cpu().double()
+    assert int(status) == 0
+    ref, a = CU.attention_ref(cache, 0, q, cu, past)
+    tol = CU.attention_tolerance(dtype, ref, a, hd, max(p + n for p, n in zip(past, news)))
+    worst = ((o - ref).abs() / tol).max().item()
+    assert torch.isfinite(o).all() and worst <= 1.0, f"worst error is {worst:.2f} of what arithmetic allows"
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("hq,kv", [(4, 4), (8, 2), (3, 1), (8, 1), (9, 1)])
+def test_neighbours_that_begin_with_the_same_pages(dtype, hd, page, hq, kv):
+    # 1280 common keys (two, then nine sequences: more than a block), 512, 256 (the least), 240 (too few); one apart in between
+    past = [1300, 1281, 600, 1400, 1290, 1280, 1283, 1300, 1500, 1281, 1282, 1290, 520, 513, 700, 260, 256, 257, 250, 249]
+    news = [1] * len(past)
+    groups = [(0, 2, 1280 // page), (3, 9, 1280 // page), (12, 3, 512 // page), (15, 3, 256 // page)]
+    if page == 16:
+        groups.append((18, 2, 15))
+    check_forks(past, news, groups, hq, kv, hd, page, dtype)
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 32)])
+def test_forks_with_several_new_tokens_of_different_number(dtype, hd):
+    past = [700, 690, 800, 640, 900, 901, 902, 903, 904, 905]
+    news = [2, 2, 3, 3, 1, 1, 4, 4, 4, 9]
+    check_forks(past, news, [(0, 10, 40)], 2, 1, hd, 16, dtype)
+    check_forks(past, news, [(0, 10, 40)], 4, 2, hd, 16, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES_16)
+def test_forks_beside_chunks(dtype):
+    past = [2000, 2001, 2002, 100, 0, 2100, 2200, 2300, 2301, 2302]
+    news = [1, 1, 1, 90, 200, 1, 1, 1, 1, 1]
+    check_forks(past, news, [(0, 3, 60), (5, 5, 60)], 8, 2, 128, 32, dtype)
+
+
+@pytest.mark.parametrize("B", [2, 65, 300, 1030])
+def test_many_forks_of_a_few_prompts(B):
+    rng = random.Random(B)
+    past, groups, b = [], [], 0
+    while b < B:
+        n = min(B - b, rng.choice([1, 2, 3, 7, 40]))
+        pages = rng.choice([16, 17, 30])
+        past += [16 * pages + rng.randint(0, 40) for _ in range(n)]
+        groups.append((b, n, pages))
+        b += n
+    check_forks(past, [1] * B, groups, 4, 2, 128, 16, "bf16")
+
+
+def test_a_long_common_prefix_is_split_and_so_is_the_rest():
+    check_forks([9000, 12000, 8200, 8192], [1] * 4, [(0, 4, 128)], 4, 1, 128, 64, "f16")
+
+
+def test_forks_that_are_not_cached_or_out_of_range():
+    # a sequence without a place, a slot out of range and a bad row range between the others
+    cache = forks(3, [600] * 5, [1] * 5, [(0, 5, 30)], 2, 128, 16, "bf16")
+    q = queries(4, 5, 4, 128, "bf16")
+    status, out = CU.status_word(), torch.full_like(queries(4, 5, 4, 128, "bf16"), 7.0)
+    attend(cache, q, [0, 1, 2, 3, 4, 5], [600, -1, 600, 600, 600], 1, slots=[0, 1, 2, 9, 4], status=status, out=out, share=True)
+    assert int(status) == BAD_SLOT and (out[1] == 0).all() and (out[3] == 0).all()
+    ref, a = CU.attention_ref(cache, 0, q, [0, 1, 2, 3, 4, 5], [600, -1, 600, -1, 600], [0, 1, 2, 3, 4])
+    assert ((out.cpu().double() - ref).abs() <= CU.attention_tolerance("bf16", ref, a, 128, 601)).all()
+    status.zero_()
+    out.fill_(7.0)
+    attend(cache, q, [0, 1, 2, 2, 9, 5], [600] * 5, 1, status=status, out=out, share=True)
+    assert int(status) == BAD_CU and torch.isfinite(out).all() and (out[2:] == 7).all()
+
+
+def test_the_same_slot_many_times_and_a_bad_entry_in_the_common_part():
+    cache = CU.random_cache(8, [700], 2, 128, 16, "f16")
+    q = queries(9, 6, 4, 128, "f16")
+    cu, past, slots = [0, 1, 2, 3, 4, 5, 6], [699, 698, 600, 699, 500, 300], [0] * 6
+    out = attend(cache, q, cu, past, 1, slots=slots, share=True)
+    ref, a = CU.attention_ref(cache, 0, q, cu, past, slots)
+    assert ((out.cpu().double() - ref).abs() <= CU.attention_tolerance("f16", ref, a, 128, 700)).all()
+    cache.page_table[0, 5] = -1
+    status = CU.status_word()
+    out = attend(cache, q, cu, past, 1, slots=slots, share=True, status=status)
+    assert int(status) == BAD_PAGE
+    cache.page_table[0, 5] = 0
+    assert torch.equal(out, attend(cache, q, cu, past, 1, slots=slots, share=True))
 
 
 def test_results_do_not_depend_on_the_run():
