@@ -401,7 +401,7 @@ int radix_cache_copy_pages(const radix_cache* cache, const int32_t* src, const i
  *                 lie in fused q | k | v rows), 16-byte aligned, strides multiples of 16 bytes
  *   cu_seqlens    int32[B+1]; rows from cu_seqlens[B] on belong to no sequence and are ignored
  * A position without a page (RADIX_ERR_BAD_PAGE), a slot out of range (RADIX_ERR_BAD_SLOT) or a range outside [0, N)
- * (RADIX_ERR_BAD_CU_SEQLENS): the token is left out and reported.  N < 2^24.
+ * (RADIX_ERR_BAD_CU_SEQLENS): the token is left out and reported.  Of two tokens for one position of a slot either is kept.  N < 2^24.
  */
 int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                        const int32_t* cu_seqlens, const int32_t* past, const int32_t* slots, int32_t B, int32_t N,

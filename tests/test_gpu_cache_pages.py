@@ -111,6 +111,29 @@ def test_many_sequences_and_more_than_a_workgroup_of_entries():
     extend(cache, pool, ws, slots, [rng.randint(0, 5) for _ in slots])
 
 
+def test_the_longest_lists():
+    n = 65535
+    cache = binding.alloc_cache(1, 1, 4, 16, 2 * n + 10, torch.float32, n + 7, 3)
+    ws = binding.alloc_workspace(binding.radix_cache_workspace_bytes(cache, n))
+    order = torch.randperm(n, device="cuda").int()
+    status = CU.status_word()
+    past = binding.radix_cache_extend(cache, torch.arange(n + 1, dtype=torch.int32, device="cuda") * 5, ws, slots=order, status=status)
+    assert int(status) == 0 and (past == 0).all() and (cache.page_refs[:n] == 1).all() and (cache.page_refs[n:] == 0).all()
+    assert torch.equal(cache.page_table[order.long(), 0], torch.arange(n, dtype=torch.int32, device="cuda"))
+    half = order[:n // 2].contiguous()
+    binding.radix_cache_free(cache, half, status=status)
+    assert int(binding.radix_cache_compact(cache, ws, status=status)) == n - n // 2 and int(status) == 0
+    kept = cache.page_table[order[n // 2:].long(), 0]
+    assert torch.equal(kept.sort().values, torch.arange(n - n // 2, dtype=torch.int32, device="cuda"))
+    binding.radix_cache_fork(cache, order[n // 2:n // 2 + n // 2].contiguous(), half, ws, status=status)
+    assert int(status) == 0 and (cache.seq_lens[order.long()] == 5).all()
+    new = cache.page_table[half.long(), 0]
+    assert torch.equal(new, torch.arange(n - n // 2, n - n // 2 + n // 2, dtype=torch.int32, device="cuda"))
+    binding.radix_cache_fork(cache, order[:1].contiguous(), torch.full((1,), n + 6, dtype=torch.int32, device="cuda"), ws, status=status)
+    past = binding.radix_cache_extend(cache, CU.i32([0, 44]), ws, slots=CU.i32([n + 6]), status=status)
+    assert int(status) == -12 and past.item() == -1                          # 5 + 44 positions in a row of 48
+
+
 @pytest.mark.parametrize("what", ["extend", "fork"])
 def test_an_exhausted_pool_changes_nothing(what):
     cache, pool, ws, pages = make(8, 16, 6, 8)

@@ -340,6 +340,67 @@ def test_offsets_beyond_32_bits():
     assert ((out - ref).abs() <= CU.attention_tolerance("bf16", ref, a, 128, 301)).all()
 
 
+@pytest.mark.parametrize("hq,kv", [(33, 1), (64, 1), (128, 2)])
+def test_groups_of_more_than_32_heads(hq, kv):
+    check([0, 700, 64, 3], [1, 1, 2, 5], hq, kv, 128, 32, "bf16")
+    check([0, 700, 64, 3], [1, 1, 1, 1], hq, kv, 128, 32, "f16")
+
+
+@pytest.mark.parametrize("dtype,hd,n", [("bf16", 128, 1), ("f16", 128, 70), ("f32", 20, 3)])
+@pytest.mark.parametrize("long", [100, 3000])
+def test_strided_outputs_leave_what_lies_between(dtype, hd, n, long):
+    cache = CU.random_cache(5, [long + n, 40 + n], 2, hd, 16, dtype)
+    q = queries(6, 2 * n, 6, hd, dtype, fused_with=3)
+    rows = torch.full((2 * n, 8 * hd), 7.0, dtype=q.dtype, device="cuda")
+    out = rows[:, hd:7 * hd].view(2 * n, 6, hd)
+    want = attend(cache, q, [0, n, 2 * n], [long, 40], n)
+    attend(cache, q, [0, n, 2 * n], [long, 40], n, out=out)
+    assert torch.equal(out, want) and (rows[:, :hd] == 7).all() and (rows[:, 7 * hd:] == 7).all()
+
+
+@pytest.mark.parametrize("share", [False, True])
+def test_65535_sequences_most_of_them_empty(share):
+    B, live = 65535, [0, 1, 2, 700, 701, 40000, 65533, 65534]
+    cache = CU.random_cache(5, [300] * len(live), 2, 128, 16, "bf16")
+    news, slots = [0] * B, [-5] * B                                          # a slot that nobody asks for is not looked at
+    for i, b in enumerate(live):
+        news[b], slots[b] = 1, i
+    q = queries(6, len(live), 4, 128, "bf16")
+    status = CU.status_word()
+    out = attend(cache, q, CU.ragged(news), [299] * B, 1, slots=slots, status=status, share=share)
+    assert int(status) == 0 and torch.equal(out, attend(cache, q, list(range(len(live) + 1)), [299] * len(live), 1))
+
+
+def test_two_calls_at_once_and_a_replayed_search():
+    cache = forks(3, [700] * 8, [1] * 8, [(0, 8, 40)], 2, 128, 16, "bf16")
+    qs = [queries(s, 8, 4, 128, "bf16") for s in (1, 2)]
+    cu, past = CU.i32(list(range(9))), CU.i32([700] * 8)
+    wss = [binding.alloc_workspace(binding.radix_paged_attention_workspace_bytes(cache, 4, 8, 8, 1, True)) for _ in qs]
+    want = [binding.radix_paged_attention(cache, 0, q, cu, past, 1, ws, find_shared=True) for q, ws in zip(qs, wss)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(5):
+        got = [binding.radix_paged_attention(cache, 0, q, cu, past, 1, ws, stream=s, find_shared=True) for q, ws, s in zip(qs, wss, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(want[0])
+    streams[0].wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(streams[0]), torch.cuda.graph(graph, stream=streams[0]):
+        binding.radix_paged_attention(cache, 0, qs[0], cu, past, 1, wss[0], out=out, find_shared=True)
+    for i in range(3):
+        out.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0])
+    # the sequences grow, and one of them leaves the others, between replays
+    cache.page_table[3, 0] = cache.page_table[3, 41]
+    past.copy_(CU.i32([690, 700, 640, 650, 660, 700, 700, 655]))
+    graph.replay()
+    torch.cuda.synchronize()
+    ref, a = CU.attention_ref(cache, 0, qs[0], list(range(9)), past.tolist())
+    assert ((out.cpu().double() - ref).abs() <= CU.attention_tolerance("bf16", ref, a, 128, 701)).all()
+
+
 def test_a_stream_of_its_own():
     cache = CU.random_cache(5, [500], 2, 128, 32, "bf16")
     q = queries(6, 1, 4, 128, "bf16")

@@ -74,6 +74,11 @@ def test_rows_that_start_anywhere(dtype, pad):
     check(torch.as_strided(whole, (6, 8900), whole.stride(), pad), tokens(1, 6, 8900, 1), 3)       # and the first one off its line
 
 
+@pytest.mark.parametrize("dtype,n,v", [("f32", 1, 3000001), ("bf16", 2, 1 << 20), ("f16", 1100, 4097)])
+def test_long_rows_and_many_given_tokens(dtype, n, v):
+    check(logits(v, n, v, dtype), tokens(v, n, v, 200 if n < 10 else 65), 7)
+
+
 @pytest.mark.parametrize("k", [1, 2, 16, 31, 32])
 @pytest.mark.parametrize("n,v", [(1, 40000), (600, 3000), (2, 33)])
 def test_numbers_of_alternatives(k, n, v):
