@@ -99,9 +99,9 @@ __device__ __forceinline__ int join_entries(bool few, int rows, int kv, int spli
 // Forks of one prompt hold the same pages, and decoding them one by one reads those once per sequence while most of a 16-row tile is
 // empty.  So sequences that stand next to each other in the batch and begin with the same pages form a cluster: their rows share tiles
 // over the common keys (all of them before any new token: nothing is masked), then each walks its own keys; the join brings both
-// together.  32 query heads over 8 kv heads, 64 tokens behind 3840 common and 160 own keys: 105 us one by one, 70 with the search for
+// together.  32 query heads over 8 kv heads, 64 tokens behind 3840 common and 160 own keys: 105 us one by one, 59 with the search for
 // clusters (12 of them its two launches, which a forward makes once for all its layers); 256 tokens of 16 heads behind 2048 and 32:
-// 181 and 83.  Nothing in common: 167 and 180.
+// 180 and 72.  Nothing in common: 167 and 179.
 //
 // One wavefront per sequence: full pages that it has in common with the one before it.
 __global__ __launch_bounds__(256) void paged_common_kernel(CacheView c, PagedShape s, PagedLayout L, const int32_t* __restrict__ cu,
@@ -442,25 +442,30 @@ template <int DT, int NT> struct FewTile {
         return {table[kk >> c.page_shift], table[kv >> c.page_shift]};
     }
     // Eight keys in a row lie in one page, so one address and offsets will do.  Rows past the end of the sequence, which its last page may
-    // have, are loaded with the others and have no part: their scores are masked, their values cleared.  Keys and values are read once:
-    // non-temporal loads, with which a plain loop reads 6.9 TB/s of a large buffer, 6.1 without.
-    static __device__ __forceinline__ u32x4 once(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
-    static __device__ __forceinline__ void load_k(K& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
+    // have, are loaded with the others and have no part: their scores are masked, their values cleared.  A sequence's keys and values are
+    // read once: non-temporal loads, with which a plain loop reads 6.9 TB/s of a large buffer, 6.1 without.  KEEP: common ones, which other
+    // clusters read too, stay in L2 (70 -> 59 us for 64 tokens behind 3840 common keys).
+    template <bool KEEP> static __device__ __forceinline__ u32x4 fetch(const char* p) {
+        const u32x4* v = reinterpret_cast<const u32x4*>(p);
+        if constexpr (KEEP) return *v;
+        return __builtin_nontemporal_load(v);
+    }
+    template <bool KEEP> static __device__ __forceinline__ void load_k(K& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
                                                   uint32_t& bad) {
         const int r = lane & 15, k0 = 32 * t + 8 * (r >> 2) + (r & 3);
         const char* p = page_at(c, base, w.pk, bad) + ((uint32_t)(k0 & (c.page_size - 1)) * 256u + 16u * (lane >> 4));
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) x.k[kb][ks] = once(p + 1024 * kb + 64 * ks);
+            for (int ks = 0; ks < 4; ++ks) x.k[kb][ks] = fetch<KEEP>(p + 1024 * kb + 64 * ks);
     }
-    static __device__ __forceinline__ void load_v(V& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
+    template <bool KEEP> static __device__ __forceinline__ void load_v(V& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
                                                   uint32_t& bad) {
         const int v0 = 32 * t + 8 * (lane >> 4);
         const char* p = page_at(c, base + (size_t)c.n_kv_heads * c.piece_bytes, w.pv, bad) +
                         ((uint32_t)(v0 & (c.page_size - 1)) * 256u + 16u * (lane & 15));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x.v[i] = once(p + 256 * i);
+        for (int i = 0; i < 8; ++i) x.v[i] = fetch<KEEP>(p + 256 * i);
     }
     static __device__ __forceinline__ void clear_past(V& x, int t, int last, int lane) {
         if (32 * t + 31 <= last) return;
@@ -524,7 +529,7 @@ template <int HC> struct FewTileF32 {                                         //
         const int p = table[min(16 * t, last) >> c.page_shift];                             // pages hold a multiple of 16 keys
         return {p, p};
     }
-    static __device__ __forceinline__ void load_k(K& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
+    template <bool KEEP> static __device__ __forceinline__ void load_k(K& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
                                                   uint32_t& bad) {
         const int g = lane >> 4;
         const float* kr = reinterpret_cast<const float*>(page_at(c, base, w.pk, bad)) +
@@ -535,7 +540,7 @@ template <int HC> struct FewTileF32 {                                         //
             if (16 * j + 4 * g < hd) x.k[j] = *reinterpret_cast<const f32x4*>(kr + 16 * j + 4 * g);
         }
     }
-    static __device__ __forceinline__ void load_v(V& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
+    template <bool KEEP> static __device__ __forceinline__ void load_v(V& x, const CacheView& c, const char* base, Where w, int t, int last, int hd, int lane,
                                                   uint32_t& bad) {
         const int r = lane & 15, g = lane >> 4;
         const float* vp = reinterpret_cast<const float*>(page_at(c, base + (size_t)c.n_kv_heads * c.piece_bytes, w.pv, bad));
@@ -578,7 +583,7 @@ template <typename Tile, int NT> struct FewShared {
     float o[4][16 * NT][MAX_HD + 4];
     float m[4][16 * NT], l[4][16 * NT];
 };
-template <typename Tile, int NT>
+template <typename Tile, int NT, bool KEEP>
 __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w, const typename Tile::T* __restrict__ q,
                                          typename Tile::T* __restrict__ out, FewShared<Tile, NT>& sh, int32_t* status) {
     typedef typename Tile::T T;
@@ -624,8 +629,8 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
     int t = t0 + wave;
     if (t < t1) {
         at = Tile::where(a.c, table, t, last, lane);
-        Tile::load_k(xk, a.c, base, at, t, last, hd, lane, bad);
-        Tile::load_v(xv, a.c, base, at, t, last, hd, lane, bad);
+        Tile::template load_k<KEEP>(xk, a.c, base, at, t, last, hd, lane, bad);
+        Tile::template load_v<KEEP>(xv, a.c, base, at, t, last, hd, lane, bad);
         if (t + 4 < t1) at = Tile::where(a.c, table, t + 4, last, lane);
     }
     for (; t < t1; t += 4) {
@@ -634,7 +639,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
         for (int nt = 0; nt < NT; ++nt) tile.scores(xk, nt, s[nt]);
         typename Tile::Where next = {};
         if (t + 8 < t1) next = Tile::where(a.c, table, t + 8, last, lane);
-        if (t + 4 < t1) Tile::load_k(xk, a.c, base, at, t + 4, last, hd, lane, bad);
+        if (t + 4 < t1) Tile::template load_k<KEEP>(xk, a.c, base, at, t + 4, last, hd, lane, bad);
         float alpha[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -665,7 +670,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
                 for (int i = 0; i < 4; ++i) acc[nt][e][i] *= alpha[nt];
         Tile::clear_past(xv, t, last, lane);
         Tile::accumulate(xv, s, acc);
-        if (t + 4 < t1) Tile::load_v(xv, a.c, base, at, t + 4, last, hd, lane, bad);
+        if (t + 4 < t1) Tile::template load_v<KEEP>(xv, a.c, base, at, t + 4, last, hd, lane, bad);
         at = next;
     }
     if (bad) set_status(status, RADIX_ERR_BAD_PAGE);
@@ -912,7 +917,9 @@ __global__ __launch_bounds__(256, Tile::WAVES) void paged_few_kernel(PagedArgs a
     __shared__ FewShared<Tile, NT> sh;
     PagedFound f;
     if (!paged_find(a, threadIdx.x & 63, f, status)) return;
-    few_rows<Tile, NT>(a, paged_item(a, f), q, out, sh, status);
+    const PagedItem w = paged_item(a, f);
+    if (w.common) few_rows<Tile, NT, true>(a, w, q, out, sh, status);
+    else few_rows<Tile, NT, false>(a, w, q, out, sh, status);
 }
 
 // Both kinds of items in one launch: the blocks of many rows first, whose work is the longer.
@@ -923,7 +930,7 @@ __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedArgs a, const 
     PagedFound f;
     if (!paged_find(a, threadIdx.x & 63, f, status)) return;
     const PagedItem w = paged_item(a, f);
-    if (__builtin_amdgcn_readfirstlane((int)f.few)) few_rows<FewTile<DT, 1>, 1>(a, w, q, out, sh.few, status);
+    if (__builtin_amdgcn_readfirstlane((int)f.few)) few_rows<FewTile<DT, 1>, 1, false>(a, w, q, out, sh.few, status);
     else many_rows<DT>(a, w, q, out, sh.many, status);
 }
 
