@@ -418,7 +418,7 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  *                 rows of query heads per kv head) and begin with the same pages, 256 positions or more, attend to those together,
  *                 so that they are read once for several sequences: forks of one prompt.  Two more launches, about 10 us.  0: not
  *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new, find_shared), 256-byte aligned
- * past[b] < 0: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position have
+ * past[b] < 0, or a row whose scores are all -inf: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position have
  * no influence; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).
  * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values.
  * A sequence whose range is not in [0, N) or longer than max_new (RADIX_ERR_BAD_CU_SEQLENS) is left out; a slot out of

@@ -222,6 +222,22 @@ def test_compaction_reports_entries_without_a_page():
     assert torch.equal(cache.pages.cpu(), pages)
 
 
+def test_compaction_of_an_empty_a_full_and_a_compact_pool():
+    cache, pool, ws, pages = make(9, 16, 3, 9)
+    assert int(binding.radix_cache_compact(cache, ws)) == pool.compact(pages) == 0
+    extend(cache, pool, ws, [1], [16 * 5])
+    assert int(binding.radix_cache_compact(cache, ws)) == pool.compact(pages) == 5
+    extend(cache, pool, ws, [2, 0], [0, 16 * 4])
+    assert int(binding.radix_cache_compact(cache, ws)) == pool.compact(pages) == 9
+    pool.agrees(cache)
+    extend(cache, pool, ws, [0, 1, 2], [0, 0, 0])
+    binding.radix_cache_free(cache, CU.i32([1]))
+    pool.free([1])
+    assert int(binding.radix_cache_compact(cache, ws)) == pool.compact(pages) == 4
+    pool.agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+
+
 def test_reset():
     cache, pool, ws, pages = make(12, 16, 3, 4)
     extend(cache, pool, ws, [0, 1, 2], [30, 30, 30])

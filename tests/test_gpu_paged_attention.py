@@ -1,4 +1,5 @@
 """Attention of new tokens over a paged cache on the GPU against softmax in 64 bits, with tolerances that count the roundings."""
+import math
 import random
 
 import pytest
@@ -118,6 +119,20 @@ def test_keys_that_are_masked_may_hold_anything():
     out = attend(cache, q, [0, 40], [50], 40)
     assert torch.equal(out[:35], clean[:35])
     assert torch.isnan(out[35:]).all()
+
+
+@pytest.mark.parametrize("dtype,hd,n", [("bf16", 128, 1), ("f16", 128, 40), ("f32", 32, 2)])
+@pytest.mark.parametrize("long", [60, 3000])
+def test_rows_whose_scores_are_all_infinitely_low(dtype, hd, n, long):
+    # keys of -inf under positive queries leave a row nothing: zeros; one finite key takes all the weight
+    cache = CU.random_cache(9, [long + n, long + n], 1, hd, 16, dtype)
+    finite = cache.pages[:, cache.page_table[1, 1].item(), 0, :, 5].clone()
+    cache.pages[:, :, 0] = -math.inf
+    cache.pages[:, cache.page_table[1, 1].item(), 0, :, 5] = finite
+    q = queries(2, 2 * n, 2, hd, dtype).abs() + 0.1
+    out = attend(cache, q, [0, n, 2 * n], [long, long], n)
+    v = cache.pages[0, cache.page_table[1, 1].item(), 1, 0, 5]
+    assert (out[:n] == 0).all() and torch.equal(out[n:], v.expand_as(out[n:]))
 
 
 def test_sequences_without_a_place_give_zeros_and_rows_behind_the_last_stay():

@@ -148,6 +148,13 @@ def test_no_token_and_tokens_out_of_range():
     assert int(status) == -7 and lp[1].isnan() and lp[3].isnan() and lp[0].isfinite()
 
 
+def test_rows_beyond_32_bits():
+    whole = torch.empty((2 << 30) + 70000, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(whole, (3, 60001), (1 << 30, 1), 3)
+    x.copy_(torch.randn((3, 60001), device="cuda") * 3)
+    check(x, tokens(1, 3, 60001, 2), 4)
+
+
 def test_entropy_alone_and_nothing_at_all():
     x = logits(1, 4, 500, "f32")
     lp, ent, ids, tlp = ask(x, None, 0)
