@@ -19,6 +19,9 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr float LOG2E = 1.4426950408889634f;
+// Differences below it count as it in the sums of d e^d: e^d is 0 there, and d may be -inf or so large (a mask of the type's lowest value)
+// that a multiple of it is, which would make a NaN of 0 d.
+constexpr float FAR = -1e4f;
 template <int N> struct Count { static constexpr int value = N; };
 constexpr int LIST = 1120;              // 64 kept entries and a batch of 16 for every lane fit
 
@@ -95,7 +98,7 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
         const float d = x.m == m ? 0.f : x.m - m;             // also where both are -inf
         const float f = __builtin_amdgcn_exp2f(d * LOG2E);
         r.s += f * x.s;
-        r.t += x.s == 0.f ? 0.f : f * fmaf(d, x.s, x.t);      // an empty part has d = -inf
+        r.t += f * fmaf(fmaxf(d, FAR), x.s, x.t);
     };
     Stat r = {m, 0.f, 0.f};
     add(a, r);
@@ -168,7 +171,7 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
         for (int u = 0; u < NE; ++u) top = fmaxf(top, e[u]);                    // invalid ones are -inf
         if (__any(top > m)) {
             const float mn = fmaxf(m, top), d = m == mn ? 0.f : m - mn, f = __builtin_amdgcn_exp2f(d * LOG2E);
-            t = s == 0.f ? 0.f : f * fmaf(d, s, t);
+            t = f * fmaf(fmaxf(d, FAR), s, t);
             s *= f;
             m = mn;
         }
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(const T* __restrict
         for (int u = 0; u < NE; ++u) {
             const float d = e[u] - use, p = __builtin_amdgcn_exp2f(d * LOG2E);
             s += p;
-            t = fmaf(fmaxf(d, -1e4f), p, t);                                    // 0 for d = -inf, where p is 0
+            t = fmaf(fmaxf(d, FAR), p, t);
         }
         if constexpr (TOP) {
             if (full && !__any(top > thr)) return;

@@ -33,7 +33,7 @@ def check(x, given, k):
 
     def near(got, want, extra):
         want = want.expand_as(got)
-        same = (got == want) | (got.isnan() & want.isnan())
+        same = (got == want.float()) | (got.isnan() & want.isnan())          # (2^129 rounds to an infinite fp32)
         ok = same | ((got.double() - want).abs() <= tol + extra + want.abs() * 2.0 ** -22)
         assert ok.all(), (got[~ok], want[~ok])
 
@@ -108,6 +108,24 @@ def test_ruled_out_tokens():
     assert lp[1].tolist() == [0.0, -math.inf] and ent[1].item() == 0.0
     assert ids[1].tolist() == [777, 0, 1, 2] and tlp[1].tolist() == [0.0] + [-math.inf] * 3        # then the ruled-out ones, lowest id first
     assert ids[3].tolist() == [5, 9, 0, 1] and abs(ent[3].item() - math.log(2)) < 1e-6
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n", [8, 600])
+@pytest.mark.parametrize("first", [False, True])
+def test_tokens_masked_with_the_lowest_value_of_the_type(dtype, n, first):
+    # differences of logits beyond the type's range, all at the start of a row (its first maximum is the mask's) or anywhere
+    x = logits(3, n, 20000, dtype)
+    low, high = torch.finfo(x.dtype).min, torch.finfo(x.dtype).max
+    if first:
+        x[:, :19000] = low
+    else:
+        x[:, torch.randperm(20000, generator=torch.Generator().manual_seed(1))[:15000].cuda()] = low
+    x[1] = low                                                               # nothing but masked: all alike
+    x[2] = low
+    x[2, 19999] = high
+    x[3, 5] = high
+    check(x, tokens(5, n, 20000, 3), 4)
 
 
 @pytest.mark.parametrize("n", [1, 600])
