@@ -366,7 +366,8 @@ int radix_cache_extend(const radix_cache* cache, const int32_t* slots, const int
  * radix_cache_fork - slot children[i] (empty) becomes what slot parents[i] is, i < n: full pages are shared, a partly
  * filled last page is copied (its filled rows, all layers).  A parent may have many children in one call.
  * Errors: RADIX_ERR_BAD_SLOT (out of range; a child that is not empty, is listed twice or is a parent too),
- * RADIX_ERR_OUT_OF_PAGES, RADIX_ERR_BAD_PAGE.
+ * RADIX_ERR_OUT_OF_PAGES, RADIX_ERR_BAD_PAGE (a length or a last page that cannot be).  A parent's full pages are not looked at
+ * beforehand: an entry that is no page is taken over as it is, and reported (RADIX_ERR_BAD_PAGE).
  */
 int radix_cache_fork(const radix_cache* cache, const int32_t* parents, const int32_t* children, int32_t n, void* ws,
                      size_t ws_bytes, int32_t* status_dev, void* stream);

@@ -178,6 +178,27 @@ def test_fork_refuses(parents, children, code):
     assert torch.equal(cache.pages.cpu(), pages)
 
 
+def test_fork_takes_over_an_entry_that_is_no_page_and_reports_it():
+    cache, pool, ws, pages = make(30, 16, 6, 4)
+    extend(cache, pool, ws, [0, 1], [40, 16])
+    pool.table[0][1] = 30                                                    # behind the pool; page 1 is lost
+    cache.page_table[0, 1] = 30
+    status = CU.status_word()
+    binding.radix_cache_fork(cache, CU.i32([0, 1]), CU.i32([2, 3]), ws, status=status)
+    assert int(status) == BAD_PAGE
+    pool.refs.append(0)                                                      # (the list's count of what is no page)
+    pool.fork([0, 1], [2, 3], pages)
+    assert pool.refs.pop() == 1
+    pool.agrees(cache)
+    assert torch.equal(cache.pages.cpu(), pages)
+    status.zero_()
+    cache.page_table[0, 2] = -1                                              # a last page that is none: nothing happens
+    pool.table[0][2] = -1
+    binding.radix_cache_fork(cache, CU.i32([1, 0]), CU.i32([4, 5]), ws, status=status)
+    assert int(status) == BAD_PAGE
+    pool.agrees(cache)
+
+
 def test_free_of_a_slot_twice_and_of_broken_rows():
     cache, pool, ws, _ = make(30, 16, 6, 4)
     extend(cache, pool, ws, [0, 1, 2], [50, 30, 5])
