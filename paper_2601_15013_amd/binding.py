@@ -612,8 +612,8 @@ def radix_score_tokens(model: Model, hidden: torch.Tensor, rows: Optional[torch.
                        top_k: int = 0, n_rows: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None
                        ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
     """radix_lm_head of hidden[rows] (or of the first n_rows rows) and radix_token_logprobs of its logits, which are not kept."""
-    if hidden.dtype != torch.float32 or not hidden.is_cuda or not hidden.is_contiguous():
-        raise TypeError("hidden must be a contiguous fp32 CUDA tensor")
+    if hidden.dtype != torch.float32 or not hidden.is_cuda or not hidden.is_contiguous() or hidden.dim() != 2 or hidden.shape[1] != model.cfg.d:
+        raise TypeError(f"hidden must be a contiguous fp32 CUDA tensor [n, {model.cfg.d}]")
     n_src = hidden.shape[0]
     n = rows.numel() if rows is not None else (n_src if n_rows is None else n_rows)
     g = _given(given, n)

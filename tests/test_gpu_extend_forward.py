@@ -153,6 +153,9 @@ def test_scoring_whole_documents_in_row_blocks():
     with pytest.raises(binding.RadixError) as err:
         binding.radix_score_tokens(live.model, hidden, None, given, binding.alloc_workspace(4096))
     assert err.value.code == -4
+    for wrong in (hidden.view(-1), hidden[:, :-1].contiguous(), hidden.view(550, 2, -1)):
+        with pytest.raises(TypeError):
+            binding.radix_score_tokens(live.model, wrong, None, None, ws, top_k=1)
     live.model.close()
     bare = harness.upload_model(live.w)
     with pytest.raises(binding.RadixError) as err:
