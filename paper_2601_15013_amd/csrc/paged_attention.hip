@@ -1066,9 +1066,10 @@ PagedLayout paged_layout(const CacheView& c, int dtype, const PagedShape& s) {
     L.members = words((size_t)B);
     size_t off = align_up(w * 4, 256);
     auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
-    // up to 16 rows a block, or 32: room for either, so that the size grows with max_new
-    L.few_acc = take((size_t)L.few_slots * L.few_rows * MAX_HD * 4);
-    L.few_ml = take((size_t)L.few_slots * L.few_rows * 8);
+    // 16 rows a block, or 32: room for either from 17 rows on, so that the size grows with max_new (32 is for 17 to 32 rows only)
+    const size_t few_room = (size_t)L.few_slots * (dtype != RADIX_F32 && most_rows > 16 ? 32 : 16);
+    L.few_acc = take(few_room * MAX_HD * 4);
+    L.few_ml = take(few_room * 8);
     L.many_acc = take((size_t)L.many_slots * MANY_ROWS * MAX_HD * 4);
     L.many_ml = take((size_t)L.many_slots * MANY_ROWS * 8);
     L.total = off;

@@ -86,6 +86,26 @@ def test_the_attention_workspace_grows_with_its_bounds(lib, dtype, share):
     assert lib.radix_paged_attention_workspace_bytes(None, 8, 1, 1, 4, 0, C.byref(n)) == NULL
 
 
+@pytest.mark.parametrize("share", [0, 1])
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("heads", [4, 8, 16, 32, 64, 256])
+def test_a_workspace_for_larger_bounds_holds_any_smaller_call(lib, dtype, share, heads):
+    n = C.c_size_t()
+    news = [0, 1, 2, 3, 4, 5, 8, 9, 16, 17, 32, 33, 200, 5000]
+    last = {}
+    for B in (0, 1, 2, 50, 127, 128, 600, 3000, 60000):
+        for N in (0, 1, 50, 128, 700, 9000, 70000):
+            sizes = []
+            for new in news:
+                assert lib.radix_paged_attention_workspace_bytes(cache(dtype=dtype), heads, N, B, new, share, C.byref(n)) == 0
+                sizes.append(n.value)
+            assert sizes == sorted(sizes), (B, N)
+            for other, small in last.items():
+                if other[0] <= B and other[1] <= N:
+                    assert all(x <= y for x, y in zip(small, sizes)), (other, (B, N))
+            last[B, N] = sizes
+
+
 def test_page_calls_refuse(lib):
     c = cache()
     odd = C.c_void_p(0x1010)

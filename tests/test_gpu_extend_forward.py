@@ -28,12 +28,13 @@ class Live:
         self.tol = TOL_F32 if cfg.dtype == "f32" else TOL_BF16
         self.page_ws = binding.alloc_workspace(binding.radix_cache_workspace_bytes(self.cache, slots))
 
-    def step(self, new):
+    def step(self, new, ws=None):
         """new: {slot: tokens}; returns the hidden states, after checking them against the oracle."""
         slots, lens = list(new), [len(t) for t in new.values()]
         tok = np.concatenate([np.asarray(t, dtype=np.int32) for t in new.values()])
-        ws = binding.alloc_workspace(binding.radix_extend_workspace_bytes(self.model, self.cache, len(tok), len(slots), max(lens)))
-        ws.fill_(0xFF)
+        if ws is None:
+            ws = binding.alloc_workspace(binding.radix_extend_workspace_bytes(self.model, self.cache, len(tok), len(slots), max(lens)))
+            ws.fill_(0xFF)
         y = binding.radix_extend_forward(self.model, self.cache, torch.from_numpy(tok).cuda(), CU.i32(CU.ragged(lens)), max(lens), ws,
                                          slots=CU.i32(slots))
         assert binding.radix_device_status(ws) == 0
@@ -81,6 +82,30 @@ def test_prompts_in_chunks_forks_and_steps_back(cfg, page, kw):
     binding.radix_cache_compact(live.cache, live.page_ws)
     live.step({s: words(rng, cfg, 1) for s in (1, 2, 3, 4, 5)})
     live.step({0: words(rng, cfg, 20), 4: words(rng, cfg, 1)})
+    live.model.close()
+
+
+@pytest.mark.parametrize("cfg", [F32, SMALL_BF16])
+def test_one_workspace_for_steps_of_all_sizes(cfg):
+    live, rng = Live(cfg, 79, 16), np.random.default_rng(6)
+    ws = binding.alloc_workspace(binding.radix_extend_workspace_bytes(live.model, live.cache, 200, 8, 120))
+    for news in [{0: 90, 1: 1, 2: 0, 3: 33}, {0: 1, 1: 0, 2: 1, 3: 1}, {5: 0, 0: 8, 3: 5}, {0: 1}, {2: 120, 0: 1}, {6: 2, 7: 2}]:
+        live.step({s: words(rng, cfg, n) for s, n in news.items()}, ws)
+    live.model.close()
+
+
+def test_workspaces_for_larger_bounds_hold_any_smaller_call():
+    live = Live(synth.ModelConfig("gen", 3, 256, 4, 2, 128, 320, 2048, "bf16", max_pos=1024), 80, 16, lm_head_mode=1)
+    last = []
+    for B in (1, 20, 128, 700):
+        for N in (1, 128, 1024, 5000):
+            sizes = [binding.radix_extend_workspace_bytes(live.model, live.cache, N, B, new) for new in (1, 2, 4, 8, 16, 17, 64, 4000)]
+            assert sizes == sorted(sizes)
+            assert all(x <= y for b, n, small in last if b <= B and n <= N for x, y in zip(small, sizes))
+            last.append((B, N, sizes))
+    for k in (0, 1, 32):
+        sizes = [binding.radix_score_tokens_workspace_bytes(live.model, n, 1, k) for n in (0, 1, 2, 15, 16, 17, 500, 512, 513, 9000)]
+        assert sizes == sorted(sizes)
     live.model.close()
 
 
