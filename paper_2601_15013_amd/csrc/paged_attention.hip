@@ -725,7 +725,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
 // fills 16 rows of a tile, which lie in one page (pages hold a multiple of 16 keys).  The products are formed as in the full-layout
 // kernel: S^T = K Q^T with 32x32x16 matrix instructions, so that a lane owns one row; O^T = V^T P^T with V^T read by transposing reads.
 // Bound as that one is, by how far matrix instructions, softmax arithmetic and LDS reads overlap: chunks of 900 to 1100 tokens behind
-// 2000 to 8000, 32 heads over 8, fp16: 430 us in a steady loop, 790 TFLOP/s.
+// 2000 to 8000, 32 heads over 8, fp16: 430 to 455 us by the card, 790 to 745 TFLOP/s.
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 struct ManyShared {
