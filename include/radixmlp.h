@@ -421,7 +421,8 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new, find_shared), 256-byte aligned
  * past[b] < 0, or a row whose scores are all -inf: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position have
  * no influence; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).
- * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values.
+ * Scores, softmax and sums are fp32; with 16-bit types the probabilities are rounded to the type before they meet the values (fp16: times
+ * 2^15, so that weights down to 2^-29 of a row's largest keep all their bits).
  * A sequence whose range is not in [0, N) or longer than max_new (RADIX_ERR_BAD_CU_SEQLENS) is left out; a slot out of
  * range (RADIX_ERR_BAD_SLOT) or more positions than a table row holds (RADIX_ERR_BAD_PAGE): zeros; a table entry that is no
  * page is read as page 0 (RADIX_ERR_BAD_PAGE).  Results are the same in every run; how a sequence's keys are split over workgroups,

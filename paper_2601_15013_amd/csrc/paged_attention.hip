@@ -4,7 +4,9 @@
 //
 // Softmax runs online (running maximum m and sum l in fp32, one pass over the keys); the fp32 accumulators of a row are rescaled when
 // m grows.  Probabilities are rounded to the operand type for the second product: the sum l is taken before that rounding, so a row's
-// error stays at half a step of the type on each term.
+// error stays at half a step of the type on each term.  fp16 has no exponents for that below 2^-14, and many small weights beside a large
+// one add up: there p, l and the accumulators are kept times 2^15, up to which the type goes, so that a weight is rounded by half a step down
+// to 2^-29 and by 2^-40 below.  The factor drops out of the quotient.
 //
 // Rows are (token, query head of a group) pairs of one kv head, so that a key tile is read once for the whole group, whatever its
 // size.  Two kernels:
@@ -407,6 +409,10 @@ __device__ __forceinline__ int part_begin(int tiles, int part, int parts) {
     return part * per + min(part, more);
 }
 
+// Probabilities of an operand type are kept times 2^WEIGHT_BITS.
+template <typename T> constexpr float WEIGHT_BITS = 0.f;
+template <> constexpr float WEIGHT_BITS<f16_t> = 15.f;
+
 // A score (in units of the exponent of two) below it is rounded in fp32 by 2^-13 at the most, which changes p by a sixth of half a step of fp16.
 constexpr float FAR = 4096.f;
 
@@ -659,7 +665,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
             float sum = 0.f;
 #pragma unroll
             for (int u = 0; u < Tile::N_KEYS; ++u) {
-                s[nt][u] = __builtin_amdgcn_exp2f((s[nt][u] - m_use) * sc);
+                s[nt][u] = __builtin_amdgcn_exp2f(fmaf(s[nt][u] - m_use, sc, WEIGHT_BITS<T>));
                 sum += s[nt][u];
             }
             l[nt] = fmaf(l[nt], alpha[nt], sum);
@@ -856,13 +862,13 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedItem& w
         // (s - m) sc by one fused operation, s sc - mc with mc = m sc rounded.  The rounding is common to a row's keys and drops out, but where
         // it reaches whole powers of two the largest p would leave the type, or all of them vanish: beyond FAR the difference is taken first.
         // (Four chunks behind 2000 to 8000 keys: 440 us without the question, 443 with it, 455 with the difference in every tile.)
-        float neg_mc = -m_use * sc;
+        float neg_mc = fmaf(-m_use, sc, WEIGHT_BITS<T>);
         if (__builtin_expect(__any(fabsf(neg_mc) > FAR), 0)) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[kb][e] -= m_use;
-            neg_mc = 0.f;
+            neg_mc = WEIGHT_BITS<T>;
         }
         float psum = 0.f;
         V8 pf[4];
