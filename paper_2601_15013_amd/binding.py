@@ -390,9 +390,13 @@ def _list(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
 
 
 def _new(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(stream)         # written there, whatever stream it was made on
+    """An output of a call on `stream`.  It is made there: what the current stream's freed tensors leave may still be written by kernels
+    in its queue, for which `stream` does not wait.  And it is held, once freed, until the current stream has done what it was given by then."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
     return t
 
 

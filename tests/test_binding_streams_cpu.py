@@ -1,0 +1,42 @@
+"""Outputs that the binding makes for a call on another stream come from that stream's memory, and are held for the current stream, which
+will read them (recorded with stand-ins for torch's calls; no GPU needed)."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2601_15013_amd import binding
+
+
+@pytest.fixture
+def events(monkeypatch):
+    seen, at = [], ["current"]
+
+    @contextlib.contextmanager
+    def stream(s):
+        before, at[0] = at[0], s
+        yield
+        at[0] = before
+
+    class Made:
+        def record_stream(self, s):
+            seen.append(("held for", s))
+
+    def empty(shape, dtype=None, device=None):
+        seen.append(("made on", at[0], shape, dtype, device))
+        return Made()
+
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: at[0])
+    monkeypatch.setattr(torch, "empty", empty)
+    return seen
+
+
+def test_an_output_for_another_stream(events):
+    binding._new((3, 4), torch.float32, "device", "side")
+    assert events == [("made on", "side", (3, 4), torch.float32, "device"), ("held for", "current")]
+
+
+def test_an_output_for_the_current_stream(events):
+    binding._new((3,), torch.int32, "device", None)
+    assert events == [("made on", "current", (3,), torch.int32, "device")]
