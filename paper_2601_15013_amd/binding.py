@@ -154,6 +154,17 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return s.cuda_stream
 
 
+def _new(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """An output of a call on `stream`.  It is made there: what the current stream's freed tensors leave may still be written by kernels
+    in its queue, for which `stream` does not wait.  And it is held, once freed, until the current stream has done what it was given by then."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _i32(t: torch.Tensor, name: str) -> torch.Tensor:
     if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous int32 CUDA tensor")
@@ -249,11 +260,11 @@ def radix_build_index(tok: torch.Tensor, pos: Optional[torch.Tensor], cu_seqlens
     N, B = tok.numel(), cu_seqlens.numel() - 1
     dev = cu_seqlens.device
     if I_scatter is None:
-        I_scatter = torch.empty(N, dtype=torch.int32, device=dev)
+        I_scatter = _new((N,), torch.int32, dev, stream)
     if I_gather is None:
-        I_gather = torch.empty(N, dtype=torch.int32, device=dev)
+        I_gather = _new((N,), torch.int32, dev, stream)
     if n_compact_dev is None:
-        n_compact_dev = torch.empty(1, dtype=torch.int32, device=dev)
+        n_compact_dev = _new((1,), torch.int32, dev, stream)
     host = C.c_int32(-1)
     rc = _lib().radix_build_index(_ptr(_i32(tok, "tok")) if N else None, _ptr(pos), _ptr(_i32(cu_seqlens, "cu_seqlens")),
                                   B, N, _ptr(I_scatter), _ptr(I_gather), _ptr(n_compact_dev),
@@ -285,7 +296,7 @@ def radix_prefill_forward(model: Model, tok: torch.Tensor, pos: Optional[torch.T
     threshold: None = RADIX_THRESHOLD_AUTO."""
     N, B = tok.numel(), cu_seqlens.numel() - 1
     if out is None:
-        out = torch.empty((N, model.cfg.d), dtype=torch.float32, device=cu_seqlens.device)
+        out = _new((N, model.cfg.d), torch.float32, cu_seqlens.device, stream)
     mode = 0 if fused_attention is None else (2 if fused_attention else 1)
     opts = radix_fwd_opts(-1.0 if threshold is None else threshold, int(force_dedup), mode, int(pad_compact_to))
     rc = _lib().radix_prefill_forward(model.handle, _ptr(tok), _ptr(pos), _ptr(cu_seqlens), B, N, max_seqlen,
@@ -312,7 +323,7 @@ def radix_prefill_forward_nodedup(model: Model, tok: torch.Tensor, pos: Optional
                                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     N, B = tok.numel(), cu_seqlens.numel() - 1
     if out is None:
-        out = torch.empty((N, model.cfg.d), dtype=torch.float32, device=cu_seqlens.device)
+        out = _new((N, model.cfg.d), torch.float32, cu_seqlens.device, stream)
     rc = _lib().radix_prefill_forward_nodedup(model.handle, _ptr(tok), _ptr(pos), _ptr(cu_seqlens), B, N, max_seqlen,
                                               _ptr(out), _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "radix_prefill_forward_nodedup")
@@ -334,7 +345,7 @@ def radix_lm_head(model: Model, hidden: torch.Tensor, rows: Optional[torch.Tenso
     n_src = hidden.shape[0]
     n = rows.numel() if rows is not None else (n_src if n_rows is None else n_rows)
     if out is None:
-        out = torch.empty((n, model.cfg.vocab), dtype=torch.float32, device=hidden.device)
+        out = _new((n, model.cfg.vocab), torch.float32, hidden.device, stream)
     rc = _lib().radix_lm_head(model.handle, _ptr(hidden), n_src, None if rows is None else _ptr(_i32(rows, "rows")), n,
                               _ptr(out), _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "radix_lm_head")
@@ -349,7 +360,7 @@ def radix_index_select_rows(src: torch.Tensor, idx: torch.Tensor, out: Optional[
     n_rows = idx.numel()
     row_bytes = (src.numel() // max(src.shape[0], 1)) * src.element_size()
     if out is None:
-        out = torch.empty((n_rows,) + tuple(src.shape[1:]), dtype=src.dtype, device=src.device)
+        out = _new((n_rows,) + tuple(src.shape[1:]), src.dtype, src.device, stream)
     rc = _lib().radix_index_select_rows(_ptr(src), src.shape[0], _ptr(_i32(idx, "idx")), n_rows, row_bytes, _ptr(out),
                                         _ptr(status), _stream(stream))
     _check(rc, "radix_index_select_rows")
@@ -387,17 +398,6 @@ def _list(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
     if _i32(t, name).numel() != n:
         raise ValueError(f"{name} has {t.numel()} entries, not {n}")
     return _ptr(t)
-
-
-def _new(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """An output of a call on `stream`.  It is made there: what the current stream's freed tensors leave may still be written by kernels
-    in its queue, for which `stream` does not wait.  And it is held, once freed, until the current stream has done what it was given by then."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream(device))
-    return t
 
 
 def _out(t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device,

@@ -1,6 +1,7 @@
 """Outputs that the binding makes for a call on another stream come from that stream's memory, and are held for the current stream, which
 will read them (recorded with stand-ins for torch's calls; no GPU needed)."""
 import contextlib
+import inspect
 
 import pytest
 import torch
@@ -40,3 +41,9 @@ def test_an_output_for_another_stream(events):
 def test_an_output_for_the_current_stream(events):
     binding._new((3,), torch.int32, "device", None)
     assert events == [("made on", "current", (3,), torch.int32, "device")]
+
+
+def test_every_call_with_a_stream_makes_its_outputs_so():
+    takes = [f for _, f in inspect.getmembers(binding, inspect.isfunction) if "stream" in inspect.signature(f).parameters]
+    assert len(takes) > 15
+    assert [f.__name__ for f in takes if "torch.empty" in inspect.getsource(f)] == ["_new"]
