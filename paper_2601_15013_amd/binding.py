@@ -172,11 +172,12 @@ def _i32(t: torch.Tensor, name: str) -> torch.Tensor:
 
 
 class Model:
-    """Owns a radix_model handle."""
+    """Owns a radix_model handle.  device: index of the device that its weights are on (None: not known)."""
 
-    def __init__(self, handle: int, cfg: radix_model_config):
+    def __init__(self, handle: int, cfg: radix_model_config, device: Optional[int] = None):
         self.handle = handle
         self.cfg = cfg
+        self.device = device
 
     @property
     def hilo_layers(self) -> int:
@@ -232,7 +233,7 @@ def radix_model_create(cfg: Any, embed: torch.Tensor, gf: torch.Tensor,
     w = radix_weights(embed.data_ptr(), gf.data_ptr(), arr, _ptr(lm_head))
     out = C.c_void_p()
     _check(_lib().radix_model_create(C.byref(c), C.byref(w), C.byref(out)), "radix_model_create")
-    return Model(out.value, c)
+    return Model(out.value, c, torch.cuda.current_device())          # (the library allocates on the current one)
 
 
 def radix_index_workspace_bytes(max_B: int) -> int:
@@ -389,6 +390,11 @@ def _same_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> Non
     for name, t in tensors.items():
         if t is not None and t.get_device() != index:
             raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
+
+
+def _model_there(model: Model, device: torch.device) -> None:
+    if model.device is not None and model.device != device.index:
+        raise ValueError(f"the model is on cuda:{model.device}, the call's tensors on {device}")
 
 
 def _list(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
@@ -563,6 +569,7 @@ def radix_extend_forward(model: Model, cache: Cache, tok: torch.Tensor, cu_seqle
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Forward of the new tokens tok[N] behind what the cache holds of their slots; returns the hidden states [N, d]."""
     N, B = _i32(tok, "tok").numel(), _i32(cu_seqlens, "cu_seqlens").numel() - 1
+    _model_there(model, cache.device)
     _same_device(cache.device, tok=tok, cu_seqlens=cu_seqlens, ws=ws, slots=slots, out=out)
     out = _out(out, "out", (N, model.cfg.d), torch.float32, cache.device, stream)
     _launch("radix_extend_forward", cache.device, stream, model.handle, cache.ref, _ptr(tok), _ptr(cu_seqlens), _list(slots,
@@ -621,6 +628,7 @@ def radix_score_tokens(model: Model, hidden: torch.Tensor, rows: Optional[torch.
     n_src = hidden.shape[0]
     n = rows.numel() if rows is not None else (n_src if n_rows is None else n_rows)
     g = _given(given, n)
+    _model_there(model, hidden.device)
     _same_device(hidden.device, rows=rows, given=given, ws=ws)
     out = _answers(n, g, max(top_k, 0), hidden.device, stream)
     _launch("radix_score_tokens", hidden.device, stream, model.handle, _ptr(hidden), n_src, _list(rows, "rows", n), n, _ptr(given), g,
