@@ -321,8 +321,8 @@ int radix_index_select_rows(const void* src, int32_t n_src_rows, const int32_t* 
  * (`slots`; NULL: slot b for entry b).  Page numbers are given out lowest first, in the order of the list, so that every
  * result is a function of the state before the call.  Lists have at most RADIX_CACHE_MAX_LIST entries.
  *
- * Errors in device data go to *status_dev (may be NULL; first error wins; the caller clears it).  extend, fork and copy are
- * all or nothing: on an error nothing has changed.
+ * Errors in device data go to *status_dev (may be NULL; first error wins; the caller clears it).  extend and copy are
+ * all or nothing: on an error nothing has changed.  So is fork, but for one error, which radix_cache_fork names.
  */
 #define RADIX_CACHE_MAX_LIST 65535
 #define RADIX_CACHE_MAX_SLOTS 262144     /* max_seqs; n_pages may be 2^28 */
@@ -366,8 +366,9 @@ int radix_cache_extend(const radix_cache* cache, const int32_t* slots, const int
  * radix_cache_fork - slot children[i] (empty) becomes what slot parents[i] is, i < n: full pages are shared, a partly
  * filled last page is copied (its filled rows, all layers).  A parent may have many children in one call.
  * Errors: RADIX_ERR_BAD_SLOT (out of range; a child that is not empty, is listed twice or is a parent too),
- * RADIX_ERR_OUT_OF_PAGES, RADIX_ERR_BAD_PAGE (a length or a last page that cannot be).  A parent's full pages are not looked at
- * beforehand: an entry that is no page is taken over as it is, and reported (RADIX_ERR_BAD_PAGE).
+ * RADIX_ERR_OUT_OF_PAGES, RADIX_ERR_BAD_PAGE (a length or a last page that cannot be); then nothing has changed.  A parent's full pages
+ * are not looked at beforehand: an entry that is no page is taken over as it is and reported (RADIX_ERR_BAD_PAGE), and the call is done all the
+ * same.
  */
 int radix_cache_fork(const radix_cache* cache, const int32_t* parents, const int32_t* children, int32_t n, void* ws,
                      size_t ws_bytes, int32_t* status_dev, void* stream);
