@@ -416,9 +416,11 @@ int radix_cache_append(const radix_cache* cache, int32_t layer, const void* k, i
  *                 multiple of n_kv_heads (query head h reads kv head h / (n_q_heads / n_kv_heads)); alignment as above;
  *                 scores are scaled by 1 / sqrt(head_dim)
  *   max_new       >= tokens of any sequence of the call (host value, sizes the grid)
- *   find_shared   1: sequences that stand next to each other in the batch, have the same number of new tokens (two of them fit 16
- *                 rows of query heads per kv head) and begin with the same pages, 256 positions or more, attend to those together,
- *                 so that they are read once for several sequences: forks of one prompt.  Two more launches, about 10 us.  0: not
+ *   find_shared   1: sequences that stand next to each other in the batch, have the same number of new tokens and begin with the same pages,
+ *                 256 positions or more, attend to those together, so that they are read once for several sequences: forks of one prompt.
+ *                 As many of them as fit a block of rows, which are pairs of a token and a query head of one kv head; it has 32 rows where
+ *                 min(max_new, N) * n_q_heads / n_kv_heads is 17 to 32 (16-bit types), otherwise 16.  Two more launches, about 10 us.  Not
+ *                 done where B * n_kv_heads is above 8192.  0: never
  *   ws            at least radix_paged_attention_workspace_bytes(cache, n_q_heads, N, B, max_new, find_shared), 256-byte aligned
  * past[b] < 0, or a row whose scores are all -inf: zeros.  Rows behind cu_seqlens[B] are left as they were.  Cache rows behind a sequence's last position have
  * no influence; a value that is not finite at a later position of the same call can reach a token (as 0 * inf).

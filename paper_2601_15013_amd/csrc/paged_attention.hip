@@ -154,7 +154,7 @@ __global__ __launch_bounds__(PT) void paged_plan_kernel(CacheView c, PagedShape 
     __shared__ int carry;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, group = s.n_q_heads / c.n_kv_heads;
     int32_t *common = plan + L.common, *lead = plan + L.lead, *shared = plan + L.shared, *members = plan + L.members;
-    // clusters: runs of sequences that have enough in common with the one before, cut where 16 rows are full
+    // clusters: runs of sequences that have enough in common with the one before, cut where a block's rows are full
     const int tile_shift = L.few_tile == 16 ? 4 : 5, enough = 256;
     auto goes_on = [&](int b) { return b > 0 && b < s.B && (long long)common[b] << c.page_shift >= enough; };
     if (tid == 0) carry = 0;
