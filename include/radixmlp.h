@@ -469,7 +469,8 @@ int radix_extend_forward(const radix_model* model, const radix_cache* cache, con
  *                 logits by the lower id
  * Logits of -inf (tokens that are ruled out) have no part in the sums.  A row without a finite logit, or with a NaN or +inf, has
  * NaN for logprobs, entropy and top_logprobs; its ids are ordered as ever, a NaN last.  n_given, top_k may be 0 (pointers NULL then).
- * Sums are fp32; how a row is summed depends on n_rows and vocab only.  n_rows < 2^24.
+ * Sums are fp32; how a row is summed, and with it the last bits, depends on n_rows, vocab, dtype and its address modulo 16 only.
+ * n_rows < 2^24.
  */
 #define RADIX_MAX_TOP_K 32
 int radix_token_logprobs_workspace_bytes(int32_t max_rows, int32_t vocab, int32_t n_given, int32_t top_k, size_t* bytes_out);
@@ -480,7 +481,8 @@ int radix_token_logprobs(const void* logits, int32_t dtype, int64_t row_stride, 
 /*
  * radix_score_tokens - radix_lm_head and radix_token_logprobs in one call, RADIX_SCORE_ROWS rows at a time, so that the logits of
  * whole documents never exist at once.  Arguments as for the two; needs a model with an LM head.  The status word of `ws` reports
- * row indices and tokens out of range.
+ * row indices and tokens out of range.  The last bits of a row's results depend on its place in the list and on n_rows (tiles of the
+ * product, how many rows are taken together, the address of its logits).
  */
 #define RADIX_SCORE_ROWS 512
 int radix_score_tokens_workspace_bytes(const radix_model* model, int32_t max_rows, int32_t n_given, int32_t top_k, size_t* bytes_out);
