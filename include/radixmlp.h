@@ -312,7 +312,8 @@ int radix_index_select_rows(const void* src, int32_t n_src_rows, const int32_t* 
  *   pages       [n_layers][n_pages][2][n_kv_heads][page_size][head_dim] in `dtype`: keys (0) and values (1), 16-byte
  *               aligned, radix_cache_bytes bytes.  A cache for a model has its layers, kv heads, head size and
  *               compute_dtype.  Shapes: page_size 16, 32, 64, 128 or 256; head_dim 128 with 16-bit types, a multiple of
- *               4 up to 128 with RADIX_F32; a page of a layer below 2^31 bytes.
+ *               4 up to 128 with RADIX_F32; a page of a layer below 2^31 bytes, all of
+ *               them below 2^63.
  *   page_refs   int32[n_pages]  number of table entries that hold the page; 0 = free
  *   page_table  int32[max_seqs][max_pages]  entry i of a row: the page with positions i * page_size ..; -1 = none
  *   seq_lens    int32[max_seqs]  positions in the cache.  A row of length n holds its pages in its first

@@ -22,7 +22,8 @@ static inline int cache_shape(const radix_cache* c, CacheView* v) {
     v->piece_bytes = (size_t)c->page_size * c->head_dim * (c->dtype == RADIX_F32 ? 4 : 2);
     v->page_bytes = 2 * (size_t)c->n_kv_heads * v->piece_bytes;
     if (v->page_bytes > INT32_MAX) return RADIX_ERR_UNSUPPORTED;
-    v->layer_bytes = (size_t)c->n_pages * v->page_bytes;
+    v->layer_bytes = (size_t)c->n_pages * v->page_bytes;                                      // below 2^59
+    if (v->layer_bytes > (size_t)INT64_MAX / (size_t)c->n_layers) return RADIX_ERR_UNSUPPORTED;
     return RADIX_OK;
 }
 
