@@ -78,7 +78,8 @@ __device__ __forceinline__ int owner_of(const int32_t* first, int n, int r) {
 }
 
 // ------------------------------------------------------------------ extend
-// Bound by the latency of its steps, one after the other: 32 sequences 4.3 us (fork 6.1, compact of 300 pages 5.3).
+// Bound by the latency of its steps, one after the other: 32 sequences 4.6 us (fork 6.2, compact of 300 pages 5.3), and in a large pool by the
+// walk over the counts from page 0 to the last page that it takes: 14 us more behind 65 000 pages in use, 226 behind a million.
 // Sequence b of the call gets room for cu[b + 1] - cu[b] more tokens.  Where its last page is partly filled and shared (a fork
 // that was shortened), the new tokens must not reach the others: it gets a page of its own, with the rows that it has.
 __global__ __launch_bounds__(PT) void cache_extend_kernel(CacheView c, const int32_t* __restrict__ slots, const int32_t* __restrict__ cu,
@@ -298,8 +299,8 @@ __global__ __launch_bounds__(PT) void cache_copy_check_kernel(CacheView c, const
 // ------------------------------------------------------------------ moves
 // The copies of a call, and beside them what it does to the table.  A wavefront copies one piece (one head's keys or values of one
 // layer of a page: consecutive bytes) of 16-byte vectors, eight in flight per lane; the pieces are dealt to the wavefronts in turn.
-// Bound by HBM.  2.3 GB pool, 0.56 GB moved: 208 us, 5.4 TB/s read and written (217 without the non-temporal accesses; a copy of 4 GB
-// by torch runs at 4.8).  Rows of 32 forks over 28 layers (69 MB, much of it read from cache): 17 us.
+// Bound by HBM.  2.3 GB pool, 0.56 GB moved: 210 us, 5.4 TB/s read and written (217 without the non-temporal accesses; a copy of 4 GB
+// by torch runs at 4.8).  Rows of 32 forks over 28 layers (69 MB, much of it read from cache): 19 us.
 enum { TABLE_NONE = 0, TABLE_FORK = 1, TABLE_REMAP = 2 };
 template <int TABLE>
 __global__ __launch_bounds__(256) void cache_move_kernel(CacheView c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
@@ -390,8 +391,8 @@ __global__ __launch_bounds__(256) void cache_reset_kernel(CacheView c) {
 
 // ------------------------------------------------------------------ append
 // One wavefront per new token: its keys and values of all heads are two runs of 16-byte vectors; each head's part goes to its piece.
-// Bound by HBM: 21 200 tokens of 8 heads of 128, fp16: 30 us, 5.8 TB/s read and written (36 with one vector in flight and plain loads).
-// 64 tokens: 3.6 us, a launch.
+// Bound by HBM: 21 200 tokens of 8 heads of 128, fp16: 31 us, 5.6 TB/s read and written (36 with one vector in flight and plain loads).
+// 64 tokens: 3.7 us, a launch.
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, int layer, const char* __restrict__ k, const char* __restrict__ v,
                                                            size_t k_stride, size_t v_stride, const int32_t* __restrict__ cu,
                                                            const int32_t* __restrict__ past, const int32_t* __restrict__ slots, int B, int N,

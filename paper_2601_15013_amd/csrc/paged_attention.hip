@@ -427,8 +427,8 @@ __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY
 // 16 bytes of each of its keys 8 g .. 8 g + 7: eight elements 8 r .. 8 r + 7 of eight keys, an 8 x 8 square that 32 byte permutes turn
 // into what the A operand wants (eight keys of one element).  So V needs no LDS to be transposed.
 //
-// Measured, kernel alone: 64 tokens behind 500 to 4000 keys, 32 heads over 8, bf16 (593 MB): 96 us, 6.2 TB/s; one token behind 131071 keys,
-// fp16 (537 MB): 81 us, 6.6 TB/s; one behind 200 keys: 7.5 us.
+// Measured, kernel alone: 64 tokens behind 500 to 4000 keys, 32 heads over 8, bf16 (593 MB): 97 us, 6.1 TB/s; one token behind 131071 keys,
+// fp16 (537 MB): 83 us, 6.5 TB/s; one behind 200 keys: 7.8 us.
 template <int DT, int NT> struct FewTile {
     static constexpr int KEYS = 32, NA = 8, WAVES = NT == 1 ? 3 : 2;          // NA: accumulators (of four) of a lane per 16 rows; WAVES: per SIMD
     typedef typename Op<DT>::T T;
@@ -453,7 +453,7 @@ template <int DT, int NT> struct FewTile {
     // Eight keys in a row lie in one page, so one address and offsets will do.  Rows past the end of the sequence, which its last page may
     // have, are loaded with the others and have no part: their scores are masked, their values cleared.  A sequence's keys and values are
     // read once: non-temporal loads, with which a plain loop reads 6.9 TB/s of a large buffer, 6.1 without.  KEEP: common ones, which other
-    // clusters read too, stay in L2 (70 -> 59 us for 64 tokens behind 3840 common keys).
+    // clusters read too, stay in L2 (70 -> 59 us for 64 tokens behind 3840 common keys); not in batches that hold chunks as well.
     template <bool KEEP> static __device__ __forceinline__ u32x4 fetch(const char* p) {
         const u32x4* v = reinterpret_cast<const u32x4*>(p);
         if constexpr (KEEP) return *v;
@@ -518,7 +518,7 @@ template <int DT, int NT> struct FewTile {
 
 // fp32: tiles of 16 keys, v_mfma_f32_16x16x4.  Step (j, u) of the first product takes element 16 j + 4 g + u of a row, so that a lane
 // reads four consecutive elements at a time; step e of the second takes key 4 g + e, the lane's own.  8 sequences of 1 to 60 tokens
-// behind 100 to 450, 4 heads of 64 over 2: 9.8 us.
+// behind 100 to 450, 4 heads of 64 over 2: 10.2 us.
 template <int HC> struct FewTileF32 {                                         // head_dim <= 64 HC, a multiple of 4
     static constexpr int KEYS = 16, NA = 4 * HC, NJ = 4 * HC, WAVES = 3;
     typedef float T;
@@ -734,7 +734,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, const PagedItem& w,
 // fills 16 rows of a tile, which lie in one page (pages hold a multiple of 16 keys).  The products are formed as in the full-layout
 // kernel: S^T = K Q^T with 32x32x16 matrix instructions, so that a lane owns one row; O^T = V^T P^T with V^T read by transposing reads.
 // Bound as that one is, by how far matrix instructions, softmax arithmetic and LDS reads overlap: chunks of 900 to 1100 tokens behind
-// 2000 to 8000, 32 heads over 8, fp16: 430 to 455 us by the card, 790 to 745 TFLOP/s.
+// 2000 to 8000, 32 heads over 8, fp16: 430 to 458 us by the card, 789 to 740 TFLOP/s.
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 struct ManyShared {
@@ -954,7 +954,7 @@ __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(PagedArgs a, const 
 }
 
 // Joins the parts of split blocks; workgroups take entries in turn.  Groups of 32 lanes, four elements a lane: with few parts a group joins a row by itself, with more
-// the eight groups take every eighth part of one row and their sums are added in order.  Bound by latency: 4.9 us for 64 sequences, 4.6 for
+// the eight groups take every eighth part of one row and their sums are added in order.  Bound by latency: 5.1 us for 64 sequences, 4.5 for
 // one in 64 parts; one wavefront a row, parts one after the other, took 6.2 and 13.7, and 47 where chunks were split.
 struct JoinArgs {
     const int32_t *cu, *first, *splits, *slot, *lead;

@@ -10,8 +10,8 @@
 // values; the rest is appended and the list cut back to k when it is long.  No order of arrival enters the result.
 //
 // Bound by the row's bytes: 16-byte non-temporal loads, one turn of 16 elements a lane ahead; a row is split over several workgroups where
-// there are few rows, whose parts a second launch joins.  2048 rows of 151936 fp32 logits: 194 us, 6.4 TB/s (209 with range checks in every
-// turn, 227 with plain loads); 8 rows: 8.7 us and 5.2 for the join.
+// there are few rows, whose parts a second launch joins.  2048 rows of 151936 fp32 logits: 199 us, 6.3 TB/s (range checks in every turn
+// cost 15 us more, plain loads 33); 8 rows: 9.8 us and 5.5 for the join.
 #include "common.h"
 #include "kernels.h"
 
