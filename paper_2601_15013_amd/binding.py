@@ -154,15 +154,24 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return s.cuda_stream
 
 
+def _new_all(outputs: Sequence[Tuple[Tuple[int, ...], torch.dtype]], device: torch.device, stream: Optional[torch.cuda.Stream]) -> Tuple[torch.Tensor, ...]:
+    """Outputs (shape, dtype) of a call on `stream`.  They are made there: what the current stream's freed tensors leave may still be written
+    by kernels in its queue, for which `stream` does not wait.  And they are held, once freed, until the current stream has done what it was
+    given by then.  (Entering a stream takes 6 us, so all are made at once.)"""
+    current = None if stream is None else torch.cuda.current_stream(device)
+    if stream == current:
+        return tuple(torch.empty(shape, dtype=dtype, device=device) for shape, dtype in outputs)
+    with torch.cuda.stream(stream):
+        made = tuple(torch.empty(shape, dtype=dtype, device=device) for shape, dtype in outputs)
+    for t in made:
+        t.record_stream(current)
+    return made
+
+
 def _new(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """An output of a call on `stream`.  It is made there: what the current stream's freed tensors leave may still be written by kernels
-    in its queue, for which `stream` does not wait.  And it is held, once freed, until the current stream has done what it was given by then."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream(device))
-    return t
+    return _new_all([(shape, dtype)], device, stream)[0]
 
 
 def _i32(t: torch.Tensor, name: str) -> torch.Tensor:
@@ -593,8 +602,7 @@ def _given(given: Optional[torch.Tensor], n: int) -> int:
 
 def _answers(n: int, n_given: int, top_k: int, dev: torch.device, stream: Optional[torch.cuda.Stream]
              ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
-    return (_new((n, n_given), torch.float32, dev, stream), _new((n,), torch.float32, dev, stream),
-            _new((n, top_k), torch.int32, dev, stream), _new((n, top_k), torch.float32, dev, stream))
+    return _new_all([((n, n_given), torch.float32), ((n,), torch.float32), ((n, top_k), torch.int32), ((n, top_k), torch.float32)], dev, stream)
 
 
 def radix_token_logprobs(logits: torch.Tensor, given: Optional[torch.Tensor], ws: torch.Tensor, top_k: int = 0,

@@ -30,6 +30,7 @@ def calls(monkeypatch):
         raise RuntimeError(LAUNCHED)
 
     monkeypatch.setattr(binding, "_launch", launch)
+    monkeypatch.setattr(binding, "_new_all", lambda outputs, device, stream: [Tensor(shape, dtype, device.index) for shape, dtype in outputs])
     monkeypatch.setattr(binding, "_new", lambda shape, dtype, device, stream: Tensor(shape, dtype, device.index))
 
     def model(index):

@@ -43,7 +43,17 @@ def test_an_output_for_the_current_stream(events):
     assert events == [("made on", "current", (3,), torch.int32, "device")]
 
 
+def test_an_output_for_the_current_stream_by_name(events):
+    binding._new((3,), torch.int32, "device", "current")
+    assert events == [("made on", "current", (3,), torch.int32, "device")]
+
+
+def test_several_outputs_are_made_at_once(events):
+    binding._new_all([((1,), torch.int32), ((2,), torch.float32)], "device", "side")
+    assert [e[:2] for e in events] == [("made on", "side")] * 2 + [("held for", "current")] * 2
+
+
 def test_every_call_with_a_stream_makes_its_outputs_so():
     takes = [f for _, f in inspect.getmembers(binding, inspect.isfunction) if "stream" in inspect.signature(f).parameters]
     assert len(takes) > 15
-    assert [f.__name__ for f in takes if "torch.empty" in inspect.getsource(f)] == ["_new"]
+    assert [f.__name__ for f in takes if "torch.empty" in inspect.getsource(f)] == ["_new", "_new_all"]
