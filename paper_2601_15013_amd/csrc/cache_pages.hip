@@ -5,7 +5,8 @@
 // workgroups ran in.  (Reference counts are changed by atomic additions, which commute.)
 //
 // The calls that decide (extend, fork, compact, the check of a copy) run in one workgroup, because they are all or nothing: they
-// look at everything, write nothing, then either write all of it or only report.  What they decide leaves as a list of moves
+// look at everything (but for the entries of a fork's full pages, which are checked as they are copied), write nothing, then either write
+// all of it or only report.  What they decide leaves as a list of moves
 // (source page, destination page, rows), and a second launch over the chip copies.
 #include "block_scan.h"
 #include "common.h"

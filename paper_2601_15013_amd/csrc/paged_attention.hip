@@ -859,7 +859,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs& a, const PagedItem& w
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float m_new = fmaxf(m_run, top), m_use = finite_or_zero(m_new);
-        // (s - m) sc by one fused operation, s sc - mc with mc = m sc rounded.  The rounding is common to a row's keys and drops out, but where
+        // (s - m) sc + WEIGHT_BITS by one fused operation, s sc - mc with mc = m sc - WEIGHT_BITS rounded.  The rounding is common to a row's keys and drops out, but where
         // it reaches whole powers of two the largest p would leave the type, or all of them vanish: beyond FAR the difference is taken first.
         // (Four chunks behind 2000 to 8000 keys: 440 us without the question, 443 with it, 455 with the difference in every tile.)
         float neg_mc = fmaf(-m_use, sc, WEIGHT_BITS<T>);
